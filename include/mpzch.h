@@ -417,6 +417,86 @@ mpzch_status_t mpzch_lookup_jagged(mpzch_group_t *g, const int64_t *const *ident
                                    int64_t *out_slots, uint8_t *out_found, void *stream);
 
 /*
+ * Embedding operators: from the slots of a remap or lookup to what a model computes with, and back.
+ *
+ * With row(s) = s mod num_rows and f = scale * 65536 / (65536 - T), T = floor(65536 * drop_p + 1/2):
+ *   mpzch_embed       out[i, j] = f * rows[row(slots[i]), j] where the mask keeps (i, j), else 0
+ *   mpzch_embed_grad  G[r, j] = f * sum of grad[i, j] over the kept (i, j) with row(slots[i]) = r
+ *   mpzch_embed_step  the same sums, applied to the rows:
+ *                       state == NULL (SGD)             w[r, :] -= lr * G[r, :]
+ *                       else     (row-wise Adagrad)     state[r] += mean_j G[r, j]^2
+ *                                                       w[r, :] -= lr * G[r, :] / (sqrt(state[r]) + eps)
+ * A negative slot is padding: its output row is zeros, its gradient row is not read, it names no row.
+ * What is dropped or padded is zero whatever the row or gradient holds there (infinities and NaN among it).
+ *
+ * Dropout.  The mask is not stored: gradient and step draw it again from the same seed.  With
+ * word(i, j) = output number i * ceil(dim / 4) + j / 4 (from 0) of the SplitMix64 generator that starts at *seed,
+ * (i, j) is dropped when bits 16 (j mod 4) .. 16 (j mod 4) + 15 of word(i, j) are below T: with probability T / 65536,
+ * and what is kept grows by the inverse of exactly that, so that the mean stays.  The seed is read on the device, so a
+ * captured graph draws a new mask in every replay whose seed has been changed.  Seeds of different calls may
+ * be consecutive numbers: streams whose seeds are less than 2^25 apart share no word among their first 2^33.
+ *
+ * slots      [dev] int64[n], 0 <= n <= MPZCH_MAX_BATCH
+ * rows       [dev] num_rows rows of dim elements of rows_type, row_stride_bytes apart (a multiple of the element size, at
+ *            least a row); num_rows >= 1, 1 <= dim <= MPZCH_MAX_DIM
+ * grad, out  [dev] n rows of dim elements of grad_type / out_type, grad_stride_bytes / out_stride_bytes apart: the
+ *            block of one table in a wider activation will do.  Element alignment is enough everywhere; dim a multiple of
+ *            8 (4 with 32-bit elements) on 16-byte boundaries is the fastest.
+ * scale      finite;  drop_p in [0, 1];  seed [dev] uint64[1], may be NULL where T is 0
+ * Products and sums are formed in 32-bit floats and rounded once, to nearest, to the type of the result; the order of a
+ * sum is determined by n, dim, the types and the positions of the row: the same call gives the same bits.
+ * No output may overlap an input (of a step: rows and state are updated in place).
+ */
+typedef enum { MPZCH_F32 = 0, MPZCH_BF16 = 1, MPZCH_F16 = 2 } mpzch_type_t;
+#define MPZCH_MAX_DIM ((int64_t)1 << 20)
+#define MPZCH_MAX_STEP_DIM 1024            /* a step has a whole row in one wavefront */
+
+/* Lookup.  Needs no scratch.  Errors: INVALID_ARG. */
+mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n,
+                           const void *rows, int32_t rows_type, int64_t num_rows, int64_t dim, int64_t row_stride_bytes,
+                           float scale, double drop_p, const int64_t *seed,
+                           void *out, int32_t out_type, int64_t out_stride_bytes, void *stream);
+
+/*
+ * The scratch of gradients and steps: a handle without configuration, for any table.  One call per handle in flight at a
+ * time, captured ones included (two graphs that share a handle must not run side by side).  The scratch is allocated by
+ * mpzch_embed_reserve, or grown by the first call that needs more (which synchronises the device, and must not be
+ * captured), on the device that is current then; a call with another device current is answered with INVALID_ARG.
+ * 16 bytes per position of max_n, and 8 per element of max_dim for each 64 positions up to 2 048 times (beyond
+ * 4 194 304 positions for each 2 048).  Errors: INVALID_ARG, ALLOC.
+ * With enough scratch the calls below only launch kernels on the given stream, whatever the slots, and may be captured.
+ */
+typedef struct mpzch_embed_s mpzch_embed_t;
+mpzch_status_t mpzch_embed_create(mpzch_embed_t **out /* [host] */);
+mpzch_status_t mpzch_embed_destroy(mpzch_embed_t *h); /* synchronises the device; NULL is accepted */
+mpzch_status_t mpzch_embed_reserve(mpzch_embed_t *h, int64_t max_n, int64_t max_dim);
+
+/*
+ * Gradient of mpzch_embed with respect to the rows, in compact form: the distinct rows that the slots name, ascending,
+ * and the sum for each.
+ * out_slots [dev] int64[out_cap], out_rows [dev] out_cap dense rows of dim elements of out_type (both may be NULL when
+ *           out_cap == 0); entries from the count on are left as they were
+ * out_count [dev] int64[1]: distinct rows; when it exceeds out_cap the lists hold the first out_cap
+ * Errors: INVALID_ARG; UNSUPPORTED for num_rows > 2^32 - 2; ALLOC, HIP.
+ */
+mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows,
+                                const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,
+                                float scale, double drop_p, const int64_t *seed,
+                                int64_t *out_slots, void *out_rows, int32_t out_type, int64_t out_cap, int64_t *out_count,
+                                void *stream);
+
+/*
+ * Optimizer step of the rows that the slots name, straight from the sums; other rows are not touched.
+ * state [dev] float[num_rows] or NULL;  lr [dev] float[1], read on the device;  eps finite and > 0 where there is a state
+ * Errors: INVALID_ARG; UNSUPPORTED for dim > MPZCH_MAX_STEP_DIM or num_rows > 2^32 - 2; ALLOC, HIP.
+ */
+mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t n,
+                                const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,
+                                float scale, double drop_p, const int64_t *seed,
+                                void *rows, int32_t rows_type, int64_t num_rows, int64_t row_stride_bytes,
+                                float *state, const float *lr, float eps, void *stream);
+
+/*
  * Per-kernel timing for benchmarks.  enable = 1: every kernel launched through the handle is
  * bracketed by HIP events on the call's stream; enable = 2: only the Pass-1 kernel of each call
  * (k_discover / k_lookup), which costs the call some eight microseconds instead of thirty;

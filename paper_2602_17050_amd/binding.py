@@ -30,6 +30,7 @@ EXPORTED = (
     "mpzch_remap_feature_ttl", "mpzch_reset_rows_multi", "mpzch_lookup_gather", "mpzch_collect_delta", "mpzch_gather_rows", "mpzch_apply_delta",
     "mpzch_remap_jagged_feature_ttl", "mpzch_lookup_jagged", "mpzch_reset_rows_jagged",
     "mpzch_remap_noalloc", "mpzch_lookup_stats", "mpzch_create_with_layout", "mpzch_remap_reset",
+    "mpzch_embed", "mpzch_embed_create", "mpzch_embed_destroy", "mpzch_embed_reserve", "mpzch_embed_grad", "mpzch_embed_step",
 )
 LAYOUT_SEPARATE, LAYOUT_RECORDS = 0, 1
 NOALLOC_MAX_BATCH = 262144
@@ -56,6 +57,7 @@ _NATIVE_CALLS = (
     "mpzch_init_tensors", "mpzch_remap", "mpzch_remap_noalloc", "mpzch_remap_reset", "mpzch_remap_feature_ttl", "mpzch_lookup",
     "mpzch_lookup_stats", "mpzch_lookup_gather", "mpzch_reset_rows", "mpzch_reset_rows_multi", "mpzch_collect_delta",
     "mpzch_gather_rows", "mpzch_apply_delta", "mpzch_remap_jagged_feature_ttl", "mpzch_lookup_jagged", "mpzch_reset_rows_jagged",
+    "mpzch_embed", "mpzch_embed_grad", "mpzch_embed_step",
 )
 
 
@@ -98,6 +100,13 @@ def load_library(path: str | None = None):
                                                    vp, ctypes.POINTER(i64), vp, vp, vp]
     lib.mpzch_reset_rows_jagged.argtypes = [vp, vp, ctypes.POINTER(i64), vp, ctypes.POINTER(_Rows), vp]
     lib.mpzch_lookup_jagged.argtypes = [vp, ctypes.POINTER(vp), vp, vp, i64, vp, vp, vp]
+    f32, f64 = ctypes.c_float, ctypes.c_double
+    lib.mpzch_embed.argtypes = [vp, i64, vp, i32, i64, i64, i64, f32, f64, vp, vp, i32, i64, vp]
+    lib.mpzch_embed_create.argtypes = [ctypes.POINTER(vp)]
+    lib.mpzch_embed_destroy.argtypes = [vp]
+    lib.mpzch_embed_reserve.argtypes = [vp, i64, i64]
+    lib.mpzch_embed_grad.argtypes = [vp, vp, i64, i64, vp, i32, i64, i64, f32, f64, vp, vp, vp, i32, i64, vp, vp]
+    lib.mpzch_embed_step.argtypes = [vp, vp, i64, vp, i32, i64, i64, f32, f64, vp, vp, i32, i64, i64, vp, vp, f32, vp]
     for name in ("mpzch_kernel_times", "mpzch_group_kernel_times"):
         getattr(lib, name).argtypes = [vp, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(i64), i32, ctypes.POINTER(i32)]
@@ -251,6 +260,46 @@ def mpzch_apply_delta(identities, slots, ids, count_dev, rows=None, delta_rows=N
     status = (_native or _load_native()).apply_delta(identities, slots, ids, count_dev, rows, delta_rows)
     if status:
         raise MpzchError(status, "mpzch_apply_delta")
+
+
+def mpzch_embed(slots, rows, out, scale: float = 1.0, drop_p: float = 0.0, seed=None):
+    """out[i] = rows[slots[i] mod len(rows)], scaled, dropped with probability drop_p and converted; zeros for a negative slot.
+    rows, out: 2-D device tensors with dense rows (float32, bfloat16 or float16 each); seed: int64[1] on the device."""
+    status = (_native or _load_native()).embed(slots, rows, out, scale, drop_p, seed)
+    if status:
+        raise MpzchError(status, "mpzch_embed")
+
+
+def mpzch_embed_create():
+    """Handle of the scratch that mpzch_embed_grad and mpzch_embed_step use (ctypes.c_void_p)."""
+    h = ctypes.c_void_p()
+    _check(load_library().mpzch_embed_create(ctypes.byref(h)), "mpzch_embed_create")
+    return h
+
+
+def mpzch_embed_destroy(handle):
+    _check(load_library().mpzch_embed_destroy(handle), "mpzch_embed_destroy")
+
+
+def mpzch_embed_reserve(handle, max_n: int, max_dim: int):
+    _check(load_library().mpzch_embed_reserve(handle, max_n, max_dim), "mpzch_embed_reserve")
+
+
+def mpzch_embed_grad(handle, slots, grad, num_rows: int, out_slots, out_rows, out_count, scale: float = 1.0,
+                     drop_p: float = 0.0, seed=None):
+    """The gradient of mpzch_embed for its output's gradient: out_slots[:k] the distinct rows that slots name, ascending,
+    out_rows[:k] their sums, out_count[0] = k."""
+    status = (_native or _load_native()).embed_grad(handle, slots, grad, num_rows, out_slots, out_rows, out_count, scale, drop_p, seed)
+    if status:
+        raise MpzchError(status, "mpzch_embed_grad")
+
+
+def mpzch_embed_step(handle, slots, grad, rows, state, lr, eps: float = 1e-8, scale: float = 1.0, drop_p: float = 0.0, seed=None):
+    """The same sums applied to the rows: SGD (state None), or row-wise Adagrad with state float32 per row; lr: float32[1] on
+    the device."""
+    status = (_native or _load_native()).embed_step(handle, slots, grad, rows, state, lr, eps, scale, drop_p, seed)
+    if status:
+        raise MpzchError(status, "mpzch_embed_step")
 
 
 def mpzch_group_create(handles):

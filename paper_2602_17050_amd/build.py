@@ -7,6 +7,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "mpzch.hip")
+EMBED_SRC = os.path.join(HERE, "csrc", "mpzch_embed.hip")
 LIB = os.path.join(HERE, "libmpzch.so")
 NATIVE_SRC = os.path.join(HERE, "csrc", "native_call.cpp")
 NATIVE = os.path.join(HERE, "_native.so")
@@ -23,10 +24,20 @@ def hipcc() -> str:
 
 def build_library(verbose: bool = False) -> str:
     """Compiles every time it is called (cross-compiles without a GPU)."""
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wall", "-Wno-unused-result",
-           SRC, "-o", LIB + ".tmp"]
+    flags = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-Wall", "-Wno-unused-result"]
+    objects, running = [], []
+    for src in (SRC, EMBED_SRC):                 # side by side
+        objects.append(os.path.splitext(src)[0] + ".o")
+        cmd = flags + ["-c", src, "-o", objects[-1]]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        running.append(subprocess.Popen(cmd))
+    failed = [p.args for p in running if p.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(1, failed[0])
+    cmd = [hipcc(), "--offload-arch=gfx950", "-shared", *objects, "-o", LIB + ".tmp"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

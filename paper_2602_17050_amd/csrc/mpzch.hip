@@ -3,6 +3,7 @@
 // where the header says so (scratch growth, descriptor upload, timing read-out, destroy).
 #include "../../include/mpzch.h"
 #include "mpzch_block_kernel.hpp"
+#include "mpzch_host.hpp"
 #include "mpzch_row_kernels.hpp"
 
 #include <cstdlib>
@@ -112,25 +113,6 @@ constexpr int64_t kLongBatch = (int64_t)1 << 24;
 constexpr int train_blocks_per_cu(int64_t n) { return n < kLongBatch ? discover_blocks_per_cu() : kDiscoverBlocksPerCuMax; }
 static_assert(3 * sizeof(uint64_t) * discover_blocks_per_cu() <= sizeof(uint32_t) * kDiscoverBlocksPerCuMax * kWavesPerBlock, "the counter words of the workgroups of a one-chunk call fit seg_cnt");
 constexpr int group_blocks_per_cu() { return 8; }
-
-// Compute units of the current device, asked once per device and process (no handle state: read-only
-// entry points take const handles).
-mpzch_status_t device_cus(int *out)
-{
-    static std::mutex mu;
-    static int cus[64] = {0};
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return MPZCH_ERR_HIP;
-    if (dev < 0 || dev >= 64) return MPZCH_ERR_UNSUPPORTED;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!cus[dev]) {
-        int n = 0;
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return MPZCH_ERR_HIP;
-        cus[dev] = n;
-    }
-    *out = cus[dev];
-    return MPZCH_OK;
-}
 
 struct Scratch {
     char *base = nullptr;
@@ -245,15 +227,6 @@ struct Scratch {
     }
 };
 
-int grid_for(int64_t items, int64_t items_per_block, int num_cus, int blocks_per_cu)
-{
-    int64_t b = (items + items_per_block - 1) / items_per_block;
-    const int64_t cap = (int64_t)num_cus * blocks_per_cu;
-    if (b > cap) b = cap;
-    if (b < 1) b = 1;
-    return (int)b;
-}
-
 static_assert(kLruLongProbe == MPZCH_MAX_PROBE_LRU, "the LRU kernels hold max_probe / 64 slots per lane");
 
 int32_t p_eff(const TableCfg &c) { return (int64_t)c.max_probe < c.num_slots ? c.max_probe : (int32_t)c.num_slots; }
@@ -272,27 +245,6 @@ TableDesc make_desc(const TableCfg &c, int64_t *I, int32_t *M, int64_t ev_begin,
     d.ev_begin = ev_begin;
     d.ev_cap = ev_cap;
     return d;
-}
-
-#define TRY(...)                                    \
-    do {                                            \
-        mpzch_status_t st__ = (__VA_ARGS__);        \
-        if (st__ != MPZCH_OK) return st__;          \
-    } while (0)
-
-// A launch without the runtime's push and pop of its configuration and a look at the last error: 2.6 instead of 2.9 us on
-// the host.  (Arguments in braces: one that does not fit its parameter, another pointer or a number that would be narrowed,
-// does not compile.)
-template <typename... P, typename... A>
-mpzch_status_t launch(void (*kernel)(P...), int grid, int block, hipStream_t s, const A &...args)
-{
-    auto go = [&](P... values) {
-        void *pointers[] = {&values...};
-        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(grid), dim3(block), pointers, 0, s);
-    };
-    if (go(P{args}...) == hipSuccess) return MPZCH_OK;
-    (void)hipGetLastError();
-    return MPZCH_ERR_HIP;
 }
 
 // two-tensor tables from this size on (1 GiB of identities, four times the memory-side cache) are probed with

@@ -1,0 +1,362 @@
+// Host side of the embedding operators of include/mpzch.h: argument checks, the scratch of the gradients, launches.
+#include "../../include/mpzch.h"
+#include "mpzch_embed_kernels.hpp"
+#include "mpzch_host.hpp"
+
+#include <cmath>
+#include <cstring>
+#include <new>
+
+using namespace mpzch;
+
+struct mpzch_embed_s {
+    char *base = nullptr;
+    int device = -1;             // that the scratch is on
+    int64_t cap_n = 0, cap_dim = 0;
+};
+
+namespace {
+
+static_assert(kF32 == MPZCH_F32 && kBf16 == MPZCH_BF16 && kF16 == MPZCH_F16, "the element types of the header");
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int pow2_at_least(int64_t x)
+{
+    int p = 1;
+    while (p < x) p *= 2;
+    return p;
+}
+int64_t element_bytes(int32_t type) { return type == MPZCH_F32 ? 4 : 2; }
+bool type_ok(int32_t type) { return type == MPZCH_F32 || type == MPZCH_BF16 || type == MPZCH_F16; }
+
+// A 2-D tensor with dense rows, aligned to its elements.
+struct Rows {
+    const void *at;
+    int32_t type;
+    int64_t dim, stride;         // elements, bytes
+    bool ok() const
+    {
+        const int64_t e = element_bytes(type);
+        return at && type_ok(type) && stride >= dim * e && stride % e == 0 && (uintptr_t)at % e == 0;
+    }
+    // the most elements, of 8, 4, 2, 1, that every row holds whole numbers of and that are aligned in memory (16 bytes will do)
+    int width() const
+    {
+        for (int v = 8; v > 1; v /= 2) {
+            const int64_t bytes = v * element_bytes(type), need = bytes < 16 ? bytes : 16;
+            if (dim % v == 0 && (uintptr_t)at % need == 0 && stride % need == 0) return v;
+        }
+        return 1;
+    }
+};
+
+// scale and dropout of a call
+bool make_mask(float scale, double drop_p, const int64_t *seed, int64_t dim, float *factor, Mask *mask)
+{
+    if (!std::isfinite(scale) || !(drop_p >= 0.0 && drop_p <= 1.0)) return false;
+    const uint32_t t = (uint32_t)std::floor(drop_p * 65536.0 + 0.5);
+    if (t && !seed) return false;
+    mask->seed = (const uint64_t *)seed;
+    mask->threshold = t;
+    mask->words = (int32_t)((dim + 3) / 4);
+    *factor = t == 65536 ? 0.f : (float)((double)scale * 65536.0 / (65536.0 - t));
+    return true;
+}
+
+// ---- lookup ---------------------------------------------------------------------------------
+template <typename TI, typename TO, int V>
+mpzch_status_t launch_embed(const EmbedArgs &a, int grid, hipStream_t s)
+{
+    return a.mask.threshold ? launch(k_embed<TI, TO, V, true>, grid, kBlock, s, a) : launch(k_embed<TI, TO, V, false>, grid, kBlock, s, a);
+}
+template <typename TI, typename TO>
+mpzch_status_t launch_embed(const EmbedArgs &a, int width, int grid, hipStream_t s)
+{
+    switch (width) {
+    case 8: return launch_embed<TI, TO, 8>(a, grid, s);
+    case 4: return launch_embed<TI, TO, 4>(a, grid, s);
+    case 2: return launch_embed<TI, TO, 2>(a, grid, s);
+    default: return launch_embed<TI, TO, 1>(a, grid, s);
+    }
+}
+template <typename TI>
+mpzch_status_t launch_embed(const EmbedArgs &a, int32_t out_type, int width, int grid, hipStream_t s)
+{
+    switch (out_type) {
+    case MPZCH_F32: return launch_embed<TI, float>(a, width, grid, s);
+    case MPZCH_BF16: return launch_embed<TI, __bf16>(a, width, grid, s);
+    default: return launch_embed<TI, _Float16>(a, width, grid, s);
+    }
+}
+
+// ---- gradient -------------------------------------------------------------------------------
+constexpr int64_t kReduceTiles = 2048;       // tiles that a long batch is cut into, until they are as long as can be
+constexpr int64_t kReduceTileMin = 64;
+
+// most tiles that a batch of up to n positions is cut into
+int64_t reduce_tiles(int64_t n)
+{
+    const int64_t some = ceil_div(n, kReduceTileMin) < kReduceTiles ? ceil_div(n, kReduceTileMin) : kReduceTiles;
+    const int64_t full = ceil_div(n, kReduceTile);
+    return some > full ? some : full;
+}
+
+struct Areas {
+    uint64_t *entries[2];
+    uint32_t *hist, *totals, *heads, *flags, *tail_index;
+    float *head, *tail;
+};
+size_t lay_out(int64_t n, int64_t dim, char *base, Areas *out)
+{
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *p = base + at;
+        at += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    const int64_t tiles = reduce_tiles(n);
+    out->entries[0] = (uint64_t *)take(8 * (size_t)n);
+    out->entries[1] = (uint64_t *)take(8 * (size_t)n);
+    out->hist = (uint32_t *)take(4 * (size_t)kDigits * (size_t)ceil_div(n, kSortTile));
+    out->totals = (uint32_t *)take(4 * (size_t)kDigits);
+    out->heads = (uint32_t *)take(4 * (size_t)tiles);
+    out->flags = (uint32_t *)take(4 * (size_t)tiles);
+    out->tail_index = (uint32_t *)take(4 * (size_t)tiles);
+    out->head = (float *)take(4 * (size_t)tiles * (size_t)dim);
+    out->tail = (float *)take(4 * (size_t)tiles * (size_t)dim);
+    return at;
+}
+
+mpzch_status_t ensure(mpzch_embed_t *h, int64_t n, int64_t dim)
+{
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return MPZCH_ERR_HIP;
+    if (h->base && h->device != dev) return MPZCH_ERR_INVALID_ARG;
+    if (h->base && n <= h->cap_n && dim <= h->cap_dim) return MPZCH_OK;
+    if (n < 1024) n = 1024;
+    if (dim < 64) dim = 64;
+    if (n < h->cap_n) n = h->cap_n;
+    if (dim < h->cap_dim) dim = h->cap_dim;
+    if (h->base) {
+        if (hipDeviceSynchronize() != hipSuccess) return MPZCH_ERR_HIP;
+        (void)hipFree(h->base);
+        h->base = nullptr;
+        h->cap_n = h->cap_dim = 0;
+    }
+    Areas areas;
+    char *base = nullptr;
+    if (hipMalloc((void **)&base, lay_out(n, dim, nullptr, &areas)) != hipSuccess) {
+        (void)hipGetLastError();
+        return MPZCH_ERR_ALLOC;
+    }
+    h->base = base;
+    h->device = dev;
+    h->cap_n = n;
+    h->cap_dim = dim;
+    return MPZCH_OK;
+}
+
+// entries in ascending order; *out: where they are
+mpzch_status_t sort_slots(const Areas &w, const int64_t *slots, int64_t n, int64_t num_rows, const uint64_t **out, hipStream_t s)
+{
+    int bits = 0;
+    while (num_rows >> bits) ++bits;             // (padding has the row num_rows)
+    const int tiles = (int)ceil_div(n, kSortTile);
+    SortSource src{slots, nullptr, row_mod(num_rows), n, 32};
+    int which = 0;
+    for (int done = 0; done < bits; done += kDigitBits, src.shift += kDigitBits, which ^= 1) {
+        uint64_t *to = w.entries[which];
+        if (done == 0) TRY(launch(k_sort_hist<true>, tiles, kBlock, s, src, w.hist));
+        else TRY(launch(k_sort_hist<false>, tiles, kBlock, s, src, w.hist));
+        TRY(launch(k_sort_scan, kDigits, kBlock, s, w.hist, w.totals, tiles));
+        if (done == 0) TRY(launch(k_sort_scatter<true>, tiles, kBlock, s, src, (const uint32_t *)w.hist, (const uint32_t *)w.totals, to));
+        else TRY(launch(k_sort_scatter<false>, tiles, kBlock, s, src, (const uint32_t *)w.hist, (const uint32_t *)w.totals, to));
+        src.entries = to;
+    }
+    *out = src.entries;
+    return MPZCH_OK;
+}
+
+template <typename TG, bool STEP>
+mpzch_status_t launch_reduce(const ReduceArgs &a, int width, bool one, int grid, hipStream_t s)
+{
+    switch (width) {
+    case 8:
+        if constexpr (sizeof(TG) == 2)
+            return one ? launch(k_reduce<TG, 8, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 8, 4, STEP>, grid, kBlock, s, a);
+        return MPZCH_ERR_UNSUPPORTED;
+    case 4: return one ? launch(k_reduce<TG, 4, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 4, 4, STEP>, grid, kBlock, s, a);
+    case 2: return one ? launch(k_reduce<TG, 2, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 2, 8, STEP>, grid, kBlock, s, a);
+    default: return one ? launch(k_reduce<TG, 1, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 1, 16, STEP>, grid, kBlock, s, a);
+    }
+}
+// pieces of a row that a lane has where there are more than lanes (the second parameters above)
+int pieces_of_lane(int width) { return width >= 4 ? 4 : 16 / width; }
+
+// Everything behind the argument checks.  `a` holds what the caller gave.
+template <bool STEP>
+mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows, const Rows &grad, int width,
+                            ReduceArgs a, hipStream_t s)
+{
+    TRY(ensure(h, n, grad.dim));
+    Areas w;
+    lay_out(h->cap_n, h->cap_dim, h->base, &w);
+    if (n > 0) TRY(sort_slots(w, slots, n, num_rows, &a.entries, s));
+    else a.entries = w.entries[0];
+
+    if (sizeof(float) * width > 16 && grad.type == MPZCH_F32) width = 4;
+    const int64_t pieces = grad.dim / width;
+    a.n = n;
+    a.num_rows = (uint32_t)num_rows;
+    a.dim = (int32_t)grad.dim;
+    a.lanes = pieces < kWave ? pow2_at_least(pieces) : kWave;
+    const int np = pieces <= kWave ? 1 : pieces_of_lane(width);
+    a.col_blocks = (int32_t)ceil_div(pieces, (int64_t)a.lanes * np);
+    const int groups = kBlock / a.lanes;
+    int64_t tile = pow2_at_least(ceil_div(n, kReduceTiles));
+    if (tile < kReduceTileMin) tile = kReduceTileMin;
+    if (tile < groups) tile = groups;
+    if (tile > kReduceTile) tile = kReduceTile;
+    a.tile = (int32_t)tile;
+    const int tiles = n > 0 ? (int)ceil_div(n, tile) : 1;
+    a.grad = (const char *)grad.at;
+    a.grad_stride = grad.stride;
+    a.flags = w.flags;
+    a.tail_index = w.tail_index;
+    a.head = w.head;
+    a.tail = w.tail;
+    a.heads = w.heads;
+    a.scanned = tiles > kReduceTiles ? 1 : 0;
+    if constexpr (!STEP) {
+        TRY(launch(k_count_heads, tiles, kBlock, s, a.entries, n, a.num_rows, a.tile, w.heads));
+        if (a.scanned) TRY(launch(k_scan_heads, 1, kBlock, s, w.heads, tiles));
+    }
+    const int grid = tiles * a.col_blocks;
+    const bool one = np == 1;
+    switch (grad.type) {
+    case MPZCH_F32: TRY(launch_reduce<float, STEP>(a, width, one, grid, s)); break;
+    case MPZCH_BF16: TRY(launch_reduce<__bf16, STEP>(a, width, one, grid, s)); break;
+    default: TRY(launch_reduce<_Float16, STEP>(a, width, one, grid, s)); break;
+    }
+    if (tiles > 1) {
+        a.lanes = grad.dim < kBlock ? pow2_at_least(grad.dim) : kBlock;
+        a.col_blocks = (int32_t)ceil_div(grad.dim, (int64_t)a.lanes * kJoinColumns);
+        TRY(launch(k_join<STEP>, tiles * a.col_blocks, kBlock, s, a, tiles));
+    }
+    return MPZCH_OK;
+}
+
+constexpr int64_t kMaxGradRows = ((int64_t)1 << 32) - 2;     // rows and the padding behind them in 32 bits, one value to spare
+
+}  // namespace
+
+extern "C" {
+
+mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n, const void *rows, int32_t rows_type, int64_t num_rows, int64_t dim,
+                           int64_t row_stride_bytes, float scale, double drop_p, const int64_t *seed,
+                           void *out, int32_t out_type, int64_t out_stride_bytes, void *stream)
+{
+    if (n < 0 || n > MPZCH_MAX_BATCH || num_rows < 1 || dim < 1 || dim > MPZCH_MAX_DIM) return MPZCH_ERR_INVALID_ARG;
+    const Rows in{rows, rows_type, dim, row_stride_bytes}, to{out, out_type, dim, out_stride_bytes};
+    EmbedArgs a;
+    if (!make_mask(scale, drop_p, seed, dim, &a.factor, &a.mask)) return MPZCH_ERR_INVALID_ARG;
+    if (n == 0 && type_ok(rows_type) && type_ok(out_type)) return MPZCH_OK;
+    if (!slots || !in.ok() || !to.ok()) return MPZCH_ERR_INVALID_ARG;
+    int width = in.width() < to.width() ? in.width() : to.width();
+    if (width == 8 && (rows_type == MPZCH_F32 || out_type == MPZCH_F32)) width = 4;
+    a.slots = slots;
+    a.n = n;
+    a.rows = (const char *)rows;
+    a.mod = row_mod(num_rows);
+    a.row_stride = row_stride_bytes;
+    a.out = (char *)out;
+    a.out_stride = out_stride_bytes;
+    a.pieces = div32((uint32_t)(dim / width));
+    hipStream_t s = (hipStream_t)stream;
+    int num_cus = 0;
+    TRY(device_cus(&num_cus));
+    const int grid = grid_for(n * a.pieces.d, kBlock * kEmbedPieces, num_cus, 32);
+    switch (rows_type) {
+    case MPZCH_F32: return launch_embed<float>(a, out_type, width, grid, s);
+    case MPZCH_BF16: return launch_embed<__bf16>(a, out_type, width, grid, s);
+    default: return launch_embed<_Float16>(a, out_type, width, grid, s);
+    }
+}
+
+mpzch_status_t mpzch_embed_create(mpzch_embed_t **out)
+{
+    if (!out) return MPZCH_ERR_INVALID_ARG;
+    *out = new (std::nothrow) mpzch_embed_s();
+    return *out ? MPZCH_OK : MPZCH_ERR_ALLOC;
+}
+
+mpzch_status_t mpzch_embed_destroy(mpzch_embed_t *h)
+{
+    if (!h) return MPZCH_OK;
+    if (h->base) {
+        (void)hipDeviceSynchronize();
+        (void)hipFree(h->base);
+    }
+    delete h;
+    return MPZCH_OK;
+}
+
+mpzch_status_t mpzch_embed_reserve(mpzch_embed_t *h, int64_t max_n, int64_t max_dim)
+{
+    if (!h || max_n < 0 || max_n > MPZCH_MAX_BATCH || max_dim < 0 || max_dim > MPZCH_MAX_DIM) return MPZCH_ERR_INVALID_ARG;
+    return ensure(h, max_n, max_dim);
+}
+
+mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows,
+                                const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,
+                                float scale, double drop_p, const int64_t *seed,
+                                int64_t *out_slots, void *out_rows, int32_t out_type, int64_t out_cap, int64_t *out_count,
+                                void *stream)
+{
+    if (!h || n < 0 || n > MPZCH_MAX_BATCH || num_rows < 1 || dim < 1 || dim > MPZCH_MAX_DIM || out_cap < 0 || !out_count)
+        return MPZCH_ERR_INVALID_ARG;
+    if (!type_ok(grad_type) || !type_ok(out_type)) return MPZCH_ERR_INVALID_ARG;
+    if (num_rows > kMaxGradRows) return MPZCH_ERR_UNSUPPORTED;
+    ReduceArgs a;
+    std::memset(&a, 0, sizeof a);
+    if (!make_mask(scale, drop_p, seed, dim, &a.factor, &a.mask)) return MPZCH_ERR_INVALID_ARG;
+    const Rows g{grad, grad_type, dim, grad_stride_bytes};
+    const Rows to{out_rows, out_type, dim, dim * element_bytes(out_type)};
+    if (n > 0 && (!slots || !g.ok())) return MPZCH_ERR_INVALID_ARG;
+    if (out_cap > 0 && (!out_slots || !to.ok())) return MPZCH_ERR_INVALID_ARG;
+    const int width = out_cap > 0 && to.width() < g.width() ? to.width() : g.width();
+    a.out_slots = out_slots;
+    a.out_count = out_count;
+    a.out_rows = (char *)out_rows;
+    a.cap = out_cap;
+    a.type = out_type;
+    return run_gradient<false>(h, slots, n, num_rows, g, width, a, (hipStream_t)stream);
+}
+
+mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t n,
+                                const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,
+                                float scale, double drop_p, const int64_t *seed,
+                                void *rows, int32_t rows_type, int64_t num_rows, int64_t row_stride_bytes,
+                                float *state, const float *lr, float eps, void *stream)
+{
+    if (!h || n < 0 || n > MPZCH_MAX_BATCH || num_rows < 1 || dim < 1 || !lr) return MPZCH_ERR_INVALID_ARG;
+    if (!type_ok(grad_type) || !type_ok(rows_type)) return MPZCH_ERR_INVALID_ARG;
+    if (num_rows > kMaxGradRows || dim > MPZCH_MAX_STEP_DIM) return MPZCH_ERR_UNSUPPORTED;
+    if (state && !(std::isfinite(eps) && eps > 0.f)) return MPZCH_ERR_INVALID_ARG;
+    ReduceArgs a;
+    std::memset(&a, 0, sizeof a);
+    if (!make_mask(scale, drop_p, seed, dim, &a.factor, &a.mask)) return MPZCH_ERR_INVALID_ARG;
+    const Rows g{grad, grad_type, dim, grad_stride_bytes}, w{rows, rows_type, dim, row_stride_bytes};
+    if (n > 0 && (!slots || !g.ok())) return MPZCH_ERR_INVALID_ARG;
+    if (!w.ok()) return MPZCH_ERR_INVALID_ARG;
+    if (n == 0) return MPZCH_OK;
+    a.rows = (char *)rows;
+    a.row_stride = row_stride_bytes / element_bytes(rows_type);
+    a.type = rows_type;
+    a.state = state;
+    a.lr = lr;
+    a.eps = eps;
+    return run_gradient<true>(h, slots, n, num_rows, g, g.width() < w.width() ? g.width() : w.width(), a, (hipStream_t)stream);
+}
+
+}  // extern "C"

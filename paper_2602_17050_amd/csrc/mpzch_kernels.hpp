@@ -31,18 +31,12 @@
 // cursor), counters are accumulated per workgroup and added to one of several copies, and evicted
 // slots are staged in LDS and appended with one reservation per workgroup.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "mpzch_common.hpp"
+
 #include <type_traits>
 
 namespace mpzch {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x3 __attribute__((ext_vector_type(3)));
-
-constexpr int kWave = 64;
-constexpr int kBlock = 256;
-constexpr int kWavesPerBlock = kBlock / kWave;
 constexpr int kMaxTables = 64;
 constexpr int kDies = 8;               // the dies of the GPU, each with an L2 of its own, take the workgroups of a launch in turn
 constexpr int kStatCount = 9;
@@ -222,14 +216,6 @@ __device__ __forceinline__ Params lookup_params(const LookupArgs<MULTI, GATHER> 
 }
 
 // ------------------------------------------------------------------ arithmetic
-__device__ __forceinline__ uint64_t mix64(uint64_t x)
-{
-    uint64_t z = x + 0x9E3779B97F4A7C15ull;
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    return z ^ (z >> 31);
-}
-
 __device__ __forceinline__ uint64_t hash_of(int64_t id, uint64_t seed) { return mix64((uint64_t)id ^ seed); }
 __device__ __forceinline__ int64_t home_of(uint64_t hash, int64_t n_slots) { return (int64_t)__umul64hi(hash, (uint64_t)n_slots); }
 __device__ __forceinline__ int64_t home_slot(int64_t id, uint64_t seed, int64_t n_slots) { return home_of(hash_of(id, seed), n_slots); }
@@ -268,7 +254,6 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int src)
     return (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
 }
 
-__device__ __forceinline__ int lane_id() { return threadIdx.x & (kWave - 1); }
 // This wavefront's number in the workgroup, in a scalar register: what follows from it (segments, chunks, loop ends) then
 // costs scalar instructions, and the loops are branches instead of masks.
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }

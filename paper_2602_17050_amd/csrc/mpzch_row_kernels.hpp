@@ -4,20 +4,6 @@
 
 namespace mpzch {
 
-// slot mod num_rows without a division: the quotient by the reciprocal floor((2^64 - 1) / num_rows) is the exact one or
-// one less for slots below 2^63.
-struct RowMod {
-    int64_t num_rows;
-    uint64_t inverse;
-};
-__host__ __device__ inline RowMod row_mod(int64_t num_rows) { return RowMod{num_rows, ~0ull / (uint64_t)num_rows}; }
-__device__ __forceinline__ int64_t row_of(const RowMod &m, int64_t slot)
-{
-    if (slot < m.num_rows) return slot;
-    const int64_t r = slot - (int64_t)(__umul64hi((uint64_t)slot, m.inverse) * (uint64_t)m.num_rows);
-    return r >= m.num_rows ? r - m.num_rows : r;
-}
-
 // The row movers give one piece (16 or 4 bytes) of a row to a lane, so that consecutive lanes move consecutive pieces.  A
 // thread takes the pieces first, first + stride, ... of all rows; which row and which piece of it follows by additions
 // (no 64-bit division per piece).  kPieces of them are under way at a time: every piece is a chain of two accesses, slot

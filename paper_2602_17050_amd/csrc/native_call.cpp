@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -22,7 +23,7 @@ struct Functions {
     F(mpzch_init_tensors) F(mpzch_remap) F(mpzch_remap_noalloc) F(mpzch_remap_reset) F(mpzch_remap_feature_ttl)      \
     F(mpzch_lookup) F(mpzch_lookup_stats) F(mpzch_lookup_gather) F(mpzch_reset_rows) F(mpzch_reset_rows_multi)       \
     F(mpzch_collect_delta) F(mpzch_gather_rows) F(mpzch_apply_delta) F(mpzch_remap_jagged_feature_ttl)               \
-    F(mpzch_lookup_jagged) F(mpzch_reset_rows_jagged)
+    F(mpzch_lookup_jagged) F(mpzch_reset_rows_jagged) F(mpzch_embed) F(mpzch_embed_grad) F(mpzch_embed_step)
 #define F(name) decltype(&::name) name = nullptr;
     MPZCH_CALLS(F)
 #undef F
@@ -320,6 +321,101 @@ PyObject *reset_rows_jagged(PyObject *const *a)
                 (const int64_t *)i64(a[3]), (const mpzch_rows_t *)r.v, stream());
 }
 
+// ---- embedding operators: every tensor on the current device, whose stream the call goes to
+void here(const at::Tensor &t)
+{
+    if (!t.is_cuda() || t.device().index() != c10::hip::current_device()) fail(PyExc_AssertionError, "tensors on the current device only");
+}
+template <typename T>
+T *dense(PyObject *o, at::ScalarType type, int64_t numel, const char *text)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    here(t);
+    if (!t.is_contiguous() || t.scalar_type() != type || (numel >= 0 && t.numel() != numel)) fail(PyExc_AssertionError, text);
+    return (T *)t.data_ptr();
+}
+int32_t type_of(const at::Tensor &t)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: return MPZCH_F32;
+    case at::kBFloat16: return MPZCH_BF16;
+    case at::kHalf: return MPZCH_F16;
+    default: fail(PyExc_AssertionError, "float32, bfloat16 or float16");
+    }
+}
+// a 2-D tensor whose rows are dense, and of as many rows as the call needs
+struct Typed {
+    void *at;
+    int32_t type;
+    int64_t n, dim, stride;
+    explicit Typed(PyObject *o)
+    {
+        const at::Tensor &t = tensor(o);
+        here(t);
+        if (t.dim() != 2 || (t.stride(1) != 1 && t.size(1) > 1)) fail(PyExc_AssertionError, "2-D tensor with dense rows expected");
+        at = t.data_ptr();
+        type = type_of(t);
+        n = t.size(0);
+        dim = t.size(1);
+        const int64_t size = (int64_t)t.element_size();
+        // (the stride of a single row says nothing)
+        stride = n > 1 ? t.stride(0) * size : dim * size;
+        if (n > 1 && stride < dim * size) fail(PyExc_AssertionError, "rows that overlap");
+    }
+};
+double real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Failed{};
+    return v;
+}
+const int64_t *seed_of(PyObject *o) { return dense<const int64_t>(o, at::kLong, 1, "seed: one int64 on the device"); }
+const int64_t *slots_of(PyObject *o, int64_t *n)
+{
+    if (o == Py_None) fail(PyExc_AssertionError, "slots: dense int64 on the device");
+    *n = tensor(o).numel();
+    return dense<const int64_t>(o, at::kLong, -1, "slots: dense int64 on the device");
+}
+
+// slots, rows, out, scale, drop_p, seed
+PyObject *embed(PyObject *const *a)
+{
+    int64_t n;
+    const int64_t *slots = slots_of(a[0], &n);
+    const Typed rows(a[1]), out(a[2]);
+    if (out.n != n || out.dim != rows.dim) fail(PyExc_AssertionError, "out: one row per slot, as long as the table's");
+    return call(g_call.mpzch_embed, slots, n, (const void *)rows.at, rows.type, rows.n, rows.dim, rows.stride, (float)real(a[3]),
+                real(a[4]), seed_of(a[5]), out.at, out.type, out.stride, stream());
+}
+// handle, slots, grad, num_rows, out_slots, out_rows, out_count, scale, drop_p, seed
+PyObject *embed_grad(PyObject *const *a)
+{
+    int64_t n;
+    const int64_t *slots = slots_of(a[1], &n);
+    const Typed grad(a[2]), rows(a[5]);
+    if (grad.n != n) fail(PyExc_AssertionError, "grad: one row per slot");
+    if (rows.dim != grad.dim || rows.stride != rows.dim * (rows.type == MPZCH_F32 ? 4 : 2)) fail(PyExc_AssertionError, "out_rows: dense rows as long as the gradient's");
+    int64_t *out_slots = dense<int64_t>(a[4], at::kLong, rows.n, "out_slots: one dense int64 per row of out_rows");
+    if (a[6] == Py_None) fail(PyExc_AssertionError, "out_count: one int64 on the device");
+    int64_t *out_count = dense<int64_t>(a[6], at::kLong, 1, "out_count: one int64 on the device");
+    return call(g_call.mpzch_embed_grad, handle<mpzch_embed_t>(a[0]), slots, n, number(a[3]), (const void *)grad.at, grad.type, grad.dim,
+                grad.stride, (float)real(a[7]), real(a[8]), seed_of(a[9]), out_slots, rows.at, rows.type, rows.n, out_count, stream());
+}
+// handle, slots, grad, rows, state, lr, eps, scale, drop_p, seed
+PyObject *embed_step(PyObject *const *a)
+{
+    int64_t n;
+    const int64_t *slots = slots_of(a[1], &n);
+    const Typed grad(a[2]), rows(a[3]);
+    if (grad.n != n || grad.dim != rows.dim) fail(PyExc_AssertionError, "grad: one row per slot, as long as the table's");
+    float *state = dense<float>(a[4], at::kFloat, rows.n, "state: one dense float32 per row");
+    const float *lr = dense<const float>(a[5], at::kFloat, 1, "lr: one float32 on the device");
+    return call(g_call.mpzch_embed_step, handle<mpzch_embed_t>(a[0]), slots, n, (const void *)grad.at, grad.type, grad.dim, grad.stride,
+                (float)real(a[7]), real(a[8]), seed_of(a[9]), rows.at, rows.type, rows.n, rows.stride, state, lr, (float)real(a[6]),
+                stream());
+}
+
 template <PyObject *(*FN)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -366,7 +462,7 @@ PyMethodDef g_methods[] = {
     METHOD(init_tensors, 3), METHOD(remap, 9), METHOD(remap_noalloc, 9), METHOD(remap_feature_ttl, 10), METHOD(remap_reset, 12),
     METHOD(lookup, 5), METHOD(lookup_stats, 6), METHOD(lookup_gather, 7), METHOD(reset_rows, 5), METHOD(reset_rows_multi, 4),
     METHOD(collect_delta, 7), METHOD(gather_rows, 4), METHOD(apply_delta, 6), METHOD(remap_jagged, 12), METHOD(lookup_jagged, 6),
-    METHOD(reset_rows_jagged, 6), {nullptr, nullptr, 0, nullptr}};
+    METHOD(reset_rows_jagged, 6), METHOD(embed, 6), METHOD(embed_grad, 10), METHOD(embed_step, 10), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

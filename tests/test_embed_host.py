@@ -1,0 +1,118 @@
+"""CPU-only checks of the embedding operators: the reference's generator against the pinned outputs, and every refusal of the
+C ABI before a device is touched."""
+import ctypes
+import math
+import os
+
+import numpy as np
+import pytest
+
+import embed_reference as ref
+from test_host_logic import binding  # noqa: F401  (the fixture)
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INVALID, UNSUPPORTED = 1, 4
+F32, BF16, F16 = 0, 1, 2
+
+
+def test_mask_words_are_splitmix64():
+    pinned = [int(x, 16) for x in open(os.path.join(ROOT, "tests", "golden", "splitmix64_seed0.txt")) if not x.startswith("#")]
+    assert ref.splitmix_outputs(0, 0, len(pinned)).tolist() == pinned
+    assert ref.splitmix_outputs(0, 2, 2).tolist() == pinned[2:4]
+    # four draws of 16 bits in a word, the lowest bits first; rows start with a word of their own
+    word = pinned[0]
+    t = [(word >> (16 * k)) & 0xFFFF for k in range(4)]
+    for k in range(4):
+        p = t[k] / 65536
+        assert ref.keep(1, 4, p, 0)[0, k] and not ref.keep(1, 4, (t[k] + 1) / 65536, 0)[0, k]
+    assert (ref.keep(3, 5, 0.5, 9)[1] == ref.keep(2, 8, 0.5, 9)[1][:5]).all()
+
+
+def test_streams_of_consecutive_seeds_stay_apart():
+    """Two seeds whose difference d is below 2^25 meet only where k * golden = d mod 2^64 with k >= 2^33: no shorter k comes
+    within 2^25 of a multiple of 2^64.  The closest approaches are at the continued fraction's denominators."""
+    golden, m = ref.GOLDEN, 1 << 64
+    a, b = golden, m
+    k0, k1 = 0, 1
+    while b % a:
+        q = b // a
+        b, a, k0, k1 = a, b % a, k1, k0 + q * k1
+        if k1 < 1 << 33:
+            assert a > 1 << 25, (k1, a)
+
+
+def test_factor_keeps_the_mean():
+    for p in (0.1, 0.5, 1 / 3):
+        t = ref.threshold(p)
+        assert abs(t / 65536 - p) <= 2 ** -17
+        assert math.isclose(ref.factor(1.0, p) * (1 - t / 65536), 1.0)
+
+
+def test_embed_refuses_bad_arguments(binding):
+    lib = binding.load_library()
+    p = ctypes.c_void_p(0x10000)                              # never dereferenced: every call below fails first
+    odd = ctypes.c_void_p(0x10001)
+
+    def embed(slots=p, n=4, rows=p, rt=F32, nr=10, dim=16, rs=64, scale=1.0, drop=0.0, seed=None, out=p, ot=F32, os_=64):
+        return lib.mpzch_embed(slots, n, rows, rt, nr, dim, rs, scale, drop, seed, out, ot, os_, None)
+
+    for bad in (dict(slots=None), dict(rows=None), dict(out=None), dict(n=-1), dict(n=(1 << 30) + 1), dict(nr=0), dict(dim=0),
+                dict(dim=(1 << 20) + 1, rs=1 << 30, os_=1 << 30), dict(rs=60), dict(os_=60), dict(rs=66), dict(rt=3), dict(rt=-1),
+                dict(ot=7), dict(rows=odd), dict(out=odd, ot=BF16), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(drop=-0.1), dict(drop=1.5), dict(drop=float("nan")), dict(drop=0.5)):
+        assert embed(**bad) == INVALID, bad
+    assert embed(n=0, slots=None, rows=None, out=None) == 0    # nothing to do
+
+
+def test_gradient_and_step_refuse_bad_arguments(binding):
+    b = binding
+    lib = b.load_library()
+    p = ctypes.c_void_p(0x10000)
+    odd = ctypes.c_void_p(0x10001)
+    h = b.mpzch_embed_create()
+
+    def grad(h=h, slots=p, n=4, nr=10, g=p, gt=F32, dim=16, gs=64, scale=1.0, drop=0.0, seed=None, os_=p, orr=p, ot=F32, cap=4, cnt=p):
+        return lib.mpzch_embed_grad(h, slots, n, nr, g, gt, dim, gs, scale, drop, seed, os_, orr, ot, cap, cnt, None)
+
+    for bad in (dict(h=None), dict(slots=None), dict(n=-1), dict(n=(1 << 30) + 1), dict(nr=0), dict(g=None), dict(gt=3), dict(gt=-1),
+                dict(dim=0), dict(dim=(1 << 20) + 1, gs=1 << 30), dict(gs=63), dict(gs=66), dict(scale=float("inf")), dict(drop=2.0),
+                dict(drop=0.1), dict(os_=None), dict(orr=None), dict(orr=odd), dict(g=odd), dict(ot=5), dict(cap=-1), dict(cnt=None)):
+        assert grad(**bad) == INVALID, bad
+    assert grad(nr=(1 << 32) - 1) == UNSUPPORTED
+
+    def step(h=h, slots=p, n=4, g=p, gt=F32, dim=16, gs=64, scale=1.0, drop=0.0, seed=None, rows=p, rt=F32, nr=10, rs=64, state=p,
+             lr=p, eps=1e-6):
+        return lib.mpzch_embed_step(h, slots, n, g, gt, dim, gs, scale, drop, seed, rows, rt, nr, rs, state, lr, eps, None)
+
+    for bad in (dict(h=None), dict(slots=None), dict(n=-1), dict(n=(1 << 30) + 1), dict(nr=0), dict(g=None), dict(gt=3), dict(dim=0),
+                dict(gs=60), dict(scale=float("nan")), dict(drop=-1.0), dict(drop=0.1), dict(rows=None), dict(rows=odd), dict(rt=9),
+                dict(rs=60), dict(rs=66), dict(lr=None), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf"))):
+        assert step(**bad) == INVALID, bad
+    assert step(dim=1025, gs=4100, rs=4100) == UNSUPPORTED
+    assert step(nr=(1 << 32) - 1) == UNSUPPORTED
+    assert step(n=0, slots=None, g=None) == 0
+    assert lib.mpzch_embed_reserve(None, 1, 1) == INVALID
+    for n, d in ((-1, 1), (1, -1), ((1 << 30) + 1, 1), (1, (1 << 20) + 1)):
+        assert lib.mpzch_embed_reserve(h, n, d) == INVALID
+    assert lib.mpzch_embed_create(None) == INVALID
+    b.mpzch_embed_destroy(h)
+    assert lib.mpzch_embed_destroy(None) == 0
+
+
+def test_reference_step_by_hand():
+    rows, state = np.array([[1.0, 2.0], [3.0, 4.0], [5.0, 6.0]]), np.array([0.0, 7.0, 1.0])
+    slots = np.array([2, 0, 5, -1, 0])                         # 5 mod 3 = 2
+    grad = np.array([[1.0, 0.0], [2.0, 2.0], [0.0, 1.0], [9.0, 9.0], [1.0, 0.0]])
+    named, total, size, terms = ref.sums(slots, grad, 3, 2.0, 0.0, 0)
+    assert named.tolist() == [0, 2] and total.tolist() == [[6.0, 4.0], [2.0, 2.0]] and terms.tolist() == [2, 2]
+    assert size.tolist() == total.tolist()
+    w, s = ref.step(rows, state, named, total, 0.5, 1e-9)
+    assert s.tolist() == [26.0, 7.0, 5.0]
+    assert np.allclose(w, [[1 - 3 / math.sqrt(26), 2 - 2 / math.sqrt(26)], [3, 4], [5 - 1 / math.sqrt(5), 6 - 1 / math.sqrt(5)]], rtol=1e-8)
+    assert ref.step(rows, None, named, total, 0.5, 0)[0].tolist() == [[-2.0, 0.0], [3.0, 4.0], [4.0, 5.0]]
+
+
+@pytest.mark.parametrize("name", ["mpzch_embed", "mpzch_embed_create", "mpzch_embed_grad", "mpzch_embed_step"])
+def test_entry_points_are_public(name):
+    import paper_2602_17050_amd as pkg
+    assert callable(getattr(pkg, name))
