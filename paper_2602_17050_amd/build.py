@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "mpzch.hip")
 EMBED_SRC = os.path.join(HERE, "csrc", "mpzch_embed.hip")
+REDUCE_SRC = os.path.join(HERE, "csrc", "mpzch_reduce.hip")       # compiled once for each size of a table's elements
 LIB = os.path.join(HERE, "libmpzch.so")
 NATIVE_SRC = os.path.join(HERE, "csrc", "native_call.cpp")
 NATIVE = os.path.join(HERE, "_native.so")
@@ -28,9 +29,10 @@ def build_library(verbose: bool = False) -> str:
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-Wall", "-Wno-unused-result"]
     objects, running = [], []
-    for src in (SRC, EMBED_SRC):                 # side by side
-        objects.append(os.path.splitext(src)[0] + ".o")
-        cmd = flags + ["-c", src, "-o", objects[-1]]
+    units = [(SRC, ""), (EMBED_SRC, "")] + [(REDUCE_SRC, size) for size in ("0", "2", "4")]
+    for src, size in units:                      # side by side
+        objects.append(f"{os.path.splitext(src)[0]}{size}.o")
+        cmd = flags + ([f"-DMPZCH_TABLE_BYTES={size}"] if size else []) + ["-c", src, "-o", objects[-1]]
         if verbose:
             print(" ".join(cmd), flush=True)
         running.append(subprocess.Popen(cmd))

@@ -1,6 +1,7 @@
 // Host side of the embedding operators of include/mpzch.h: argument checks, the scratch of the gradients, launches.
 #include "../../include/mpzch.h"
-#include "mpzch_embed_kernels.hpp"
+#include "mpzch_reduce.hpp"
+#include "mpzch_sort.hpp"
 #include "mpzch_host.hpp"
 
 #include <cmath>
@@ -90,22 +91,75 @@ mpzch_status_t launch_embed(const EmbedArgs &a, int32_t out_type, int width, int
 }
 
 // ---- gradient -------------------------------------------------------------------------------
-constexpr int64_t kReduceTiles = 2048;       // tiles that a long batch is cut into, until they are as long as can be
-constexpr int64_t kReduceTileMin = 64;
+// How the sums are shared out: kReduceWaves wavefronts or more, but no part of a tile shorter than kPartMin entries and no
+// tile longer than kReduceTile.
+constexpr int64_t kReduceWaves = 8192;
+constexpr int kPartMin = 4;
+constexpr int64_t kTilesAdded = 2048;        // up to which a workgroup itself adds up the heads of the tiles before its own
+constexpr int64_t kWideDigits = 1 << 17;
 
-// most tiles that a batch of up to n positions is cut into
-int64_t reduce_tiles(int64_t n)
+struct ReducePlan {
+    int lanes, pieces, col_blocks, tile, tiles;      // pieces: of a lane, as compiled
+};
+// pieces of a row that a lane has where there are more of them than lanes
+int many_pieces(int width) { return 16 / width; }
+ReducePlan reduce_plan(int64_t n, int64_t dim, int width)
 {
-    const int64_t some = ceil_div(n, kReduceTileMin) < kReduceTiles ? ceil_div(n, kReduceTileMin) : kReduceTiles;
+    ReducePlan p;
+    const int64_t pieces = dim / width;
+    p.lanes = pieces < kWave ? pow2_at_least(pieces) : kWave;
+    p.pieces = pieces <= kWave ? 1 : many_pieces(width);
+    p.col_blocks = (int)ceil_div(pieces, (int64_t)p.lanes * p.pieces);
+    const int groups = kBlock / p.lanes;
+    int64_t per = ceil_div(n * p.lanes * p.col_blocks, kWave * kReduceWaves);
+    if (per < kPartMin) per = kPartMin;
+    if (per > kReduceTile / groups) per = kReduceTile / groups;
+    p.tile = (int)per * groups;
+    p.tiles = n > 0 ? (int)ceil_div(n, p.tile) : 1;
+    return p;
+}
+// most tiles, and most columns' blocks, of any batch of up to n positions and rows of up to dim elements: the parts are as
+// short as the number of wavefronts allows (kReduceWaves / kWavesPerBlock tiles), or the tiles as long as can be
+int64_t most_tiles(int64_t n)
+{
+    const int64_t some = ceil_div(n, 4 * kPartMin) < kReduceWaves / kWavesPerBlock ? ceil_div(n, 4 * kPartMin) : kReduceWaves / kWavesPerBlock;
     const int64_t full = ceil_div(n, kReduceTile);
-    return some > full ? some : full;
+    return 1 + (some > full ? some : full);
+}
+int64_t most_col_blocks(int64_t dim) { return ceil_div(dim, kWave * 16); }
+
+// How a batch is sorted: by its ranks, or in passes over tiles.
+constexpr int kFewTiles = 64;
+struct SortPlan {
+    int passes, bits, items, tiles;
+};
+SortPlan sort_plan(int64_t n, int64_t num_rows)
+{
+    int bits = 0;
+    while (num_rows >> bits) ++bits;             // (padding has the row num_rows)
+    const int widest = n <= kWideDigits ? kMaxDigitBits : 9;
+    SortPlan p;
+    p.passes = (int)ceil_div(bits, widest);
+    p.bits = (int)ceil_div(bits, p.passes);
+    if (p.bits < 6) p.bits = 6;
+    p.items = n <= kWideDigits ? 4 : 8;
+    p.tiles = (int)ceil_div(n, kSortBlock * p.items);
+    return p;
+}
+// words of the histograms (and twice that, and a tile more, of their scan) that any batch of up to n positions needs
+int64_t hist_words(int64_t n)
+{
+    const int64_t wide = ceil_div(n < kWideDigits ? n : kWideDigits, kSortBlock * 4) * (kMaxDigits / 2);
+    const int64_t narrow = ceil_div(n, kSortBlock * 8) * (512 / 2);
+    return wide > narrow ? wide : narrow;
 }
 
 struct Areas {
     uint64_t *entries[2];
-    uint32_t *hist, *totals, *heads, *flags, *tail_index;
+    uint32_t *hist, *before, *heads, *tail_index, *arrived;
     float *head, *tail;
 };
+size_t arrived_bytes(int64_t n, int64_t dim) { return 4 * (size_t)most_tiles(n) * (size_t)most_col_blocks(dim); }
 size_t lay_out(int64_t n, int64_t dim, char *base, Areas *out)
 {
     size_t at = 0;
@@ -114,14 +168,14 @@ size_t lay_out(int64_t n, int64_t dim, char *base, Areas *out)
         at += (bytes + 255) & ~(size_t)255;
         return p;
     };
-    const int64_t tiles = reduce_tiles(n);
+    const int64_t tiles = most_tiles(n);
     out->entries[0] = (uint64_t *)take(8 * (size_t)n);
     out->entries[1] = (uint64_t *)take(8 * (size_t)n);
-    out->hist = (uint32_t *)take(4 * (size_t)kDigits * (size_t)ceil_div(n, kSortTile));
-    out->totals = (uint32_t *)take(4 * (size_t)kDigits);
+    out->hist = (uint32_t *)take(4 * (size_t)hist_words(n));
+    out->before = (uint32_t *)take(8 * ((size_t)hist_words(n) + kMaxDigits / 2));
     out->heads = (uint32_t *)take(4 * (size_t)tiles);
-    out->flags = (uint32_t *)take(4 * (size_t)tiles);
     out->tail_index = (uint32_t *)take(4 * (size_t)tiles);
+    out->arrived = (uint32_t *)take(arrived_bytes(n, dim));
     out->head = (float *)take(4 * (size_t)tiles * (size_t)dim);
     out->tail = (float *)take(4 * (size_t)tiles * (size_t)dim);
     return at;
@@ -149,6 +203,12 @@ mpzch_status_t ensure(mpzch_embed_t *h, int64_t n, int64_t dim)
         (void)hipGetLastError();
         return MPZCH_ERR_ALLOC;
     }
+    lay_out(n, dim, base, &areas);
+    // the counters are zero between the calls; this is the only clear
+    if (hipMemset(areas.arrived, 0, arrived_bytes(n, dim)) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
+        (void)hipFree(base);
+        return MPZCH_ERR_HIP;
+    }
     h->base = base;
     h->device = dev;
     h->cap_n = n;
@@ -156,42 +216,38 @@ mpzch_status_t ensure(mpzch_embed_t *h, int64_t n, int64_t dim)
     return MPZCH_OK;
 }
 
+template <bool FIRST>
+mpzch_status_t sort_pass(const Areas &w, const SortPlan &p, const SortSource &src, uint64_t *to, hipStream_t s)
+{
+    const bool few = p.tiles <= kFewTiles;
+    if (p.items == 4) TRY(launch(k_sort_hist<FIRST, 4>, p.tiles, kSortBlock, s, src, w.hist));
+    else TRY(launch(k_sort_hist<FIRST, 8>, p.tiles, kSortBlock, s, src, w.hist));
+    if (!few) TRY(launch(k_sort_scan, 1 << (p.bits - 6), kSortBlock, s, (const uint32_t *)w.hist, w.before, p.tiles, src.bits));
+    const uint32_t *before = few ? nullptr : w.before;
+    if (p.items == 4) TRY(launch(k_sort_scatter<FIRST, 4>, p.tiles, kSortBlock, s, src, (const uint32_t *)w.hist, before, p.tiles, to));
+    else TRY(launch(k_sort_scatter<FIRST, 8>, p.tiles, kSortBlock, s, src, (const uint32_t *)w.hist, before, p.tiles, to));
+    return MPZCH_OK;
+}
+
 // entries in ascending order; *out: where they are
 mpzch_status_t sort_slots(const Areas &w, const int64_t *slots, int64_t n, int64_t num_rows, const uint64_t **out, hipStream_t s)
 {
-    int bits = 0;
-    while (num_rows >> bits) ++bits;             // (padding has the row num_rows)
-    const int tiles = (int)ceil_div(n, kSortTile);
-    SortSource src{slots, nullptr, row_mod(num_rows), n, 32};
-    int which = 0;
-    for (int done = 0; done < bits; done += kDigitBits, src.shift += kDigitBits, which ^= 1) {
-        uint64_t *to = w.entries[which];
-        if (done == 0) TRY(launch(k_sort_hist<true>, tiles, kBlock, s, src, w.hist));
-        else TRY(launch(k_sort_hist<false>, tiles, kBlock, s, src, w.hist));
-        TRY(launch(k_sort_scan, kDigits, kBlock, s, w.hist, w.totals, tiles));
-        if (done == 0) TRY(launch(k_sort_scatter<true>, tiles, kBlock, s, src, (const uint32_t *)w.hist, (const uint32_t *)w.totals, to));
-        else TRY(launch(k_sort_scatter<false>, tiles, kBlock, s, src, (const uint32_t *)w.hist, (const uint32_t *)w.totals, to));
+    SortSource src{slots, nullptr, row_mod(num_rows), n, 32, 0};
+    if (n <= kRankMax) {
+        *out = w.entries[0];
+        return launch(k_sort_rank, (int)ceil_div(n, kWave), kSortBlock, s, slots, src.mod, (int32_t)n, w.entries[0]);
+    }
+    const SortPlan p = sort_plan(n, num_rows);
+    src.bits = p.bits;
+    for (int k = 0; k < p.passes; ++k, src.shift += p.bits) {
+        uint64_t *to = w.entries[k & 1];
+        if (k == 0) TRY(sort_pass<true>(w, p, src, to, s));
+        else TRY(sort_pass<false>(w, p, src, to, s));
         src.entries = to;
     }
     *out = src.entries;
     return MPZCH_OK;
 }
-
-template <typename TG, bool STEP>
-mpzch_status_t launch_reduce(const ReduceArgs &a, int width, bool one, int grid, hipStream_t s)
-{
-    switch (width) {
-    case 8:
-        if constexpr (sizeof(TG) == 2)
-            return one ? launch(k_reduce<TG, 8, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 8, 4, STEP>, grid, kBlock, s, a);
-        return MPZCH_ERR_UNSUPPORTED;
-    case 4: return one ? launch(k_reduce<TG, 4, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 4, 4, STEP>, grid, kBlock, s, a);
-    case 2: return one ? launch(k_reduce<TG, 2, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 2, 8, STEP>, grid, kBlock, s, a);
-    default: return one ? launch(k_reduce<TG, 1, 1, STEP>, grid, kBlock, s, a) : launch(k_reduce<TG, 1, 16, STEP>, grid, kBlock, s, a);
-    }
-}
-// pieces of a row that a lane has where there are more than lanes (the second parameters above)
-int pieces_of_lane(int width) { return width >= 4 ? 4 : 16 / width; }
 
 // Everything behind the argument checks.  `a` holds what the caller gave.
 template <bool STEP>
@@ -204,46 +260,31 @@ mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, i
     if (n > 0) TRY(sort_slots(w, slots, n, num_rows, &a.entries, s));
     else a.entries = w.entries[0];
 
-    if (sizeof(float) * width > 16 && grad.type == MPZCH_F32) width = 4;
-    const int64_t pieces = grad.dim / width;
+    if (width == 8 && grad.type == MPZCH_F32) width = 4;
+    const ReducePlan p = reduce_plan(n, grad.dim, width);
     a.n = n;
     a.num_rows = (uint32_t)num_rows;
     a.dim = (int32_t)grad.dim;
-    a.lanes = pieces < kWave ? pow2_at_least(pieces) : kWave;
-    const int np = pieces <= kWave ? 1 : pieces_of_lane(width);
-    a.col_blocks = (int32_t)ceil_div(pieces, (int64_t)a.lanes * np);
-    const int groups = kBlock / a.lanes;
-    int64_t tile = pow2_at_least(ceil_div(n, kReduceTiles));
-    if (tile < kReduceTileMin) tile = kReduceTileMin;
-    if (tile < groups) tile = groups;
-    if (tile > kReduceTile) tile = kReduceTile;
-    a.tile = (int32_t)tile;
-    const int tiles = n > 0 ? (int)ceil_div(n, tile) : 1;
+    a.tiles = p.tiles;
+    a.tile = p.tile;
+    a.lanes = p.lanes;
+    a.col_blocks = p.col_blocks;
     a.grad = (const char *)grad.at;
     a.grad_stride = grad.stride;
-    a.flags = w.flags;
     a.tail_index = w.tail_index;
+    a.arrived = w.arrived;
     a.head = w.head;
     a.tail = w.tail;
     a.heads = w.heads;
-    a.scanned = tiles > kReduceTiles ? 1 : 0;
-    if constexpr (!STEP) {
-        TRY(launch(k_count_heads, tiles, kBlock, s, a.entries, n, a.num_rows, a.tile, w.heads));
-        if (a.scanned) TRY(launch(k_scan_heads, 1, kBlock, s, w.heads, tiles));
+    const int grid = p.tiles * p.col_blocks;
+    if constexpr (STEP) {
+        return a.type == MPZCH_F32 ? launch_reduce_4(a, grad.type, width, p.pieces, grid, s) : launch_reduce_2(a, grad.type, width, p.pieces, grid, s);
+    } else {
+        a.heads_are = n <= kRankMax ? kCountHere : p.tiles <= kTilesAdded ? kOfTile : kBeforeTile;
+        if (a.heads_are != kCountHere) TRY(launch(k_count_heads, p.tiles, kBlock, s, a.entries, n, a.num_rows, a.tile, w.heads));
+        if (a.heads_are == kBeforeTile) TRY(launch(k_scan_heads, 1, kSortBlock, s, w.heads, p.tiles));
+        return launch_reduce_0(a, grad.type, width, p.pieces, grid, s);
     }
-    const int grid = tiles * a.col_blocks;
-    const bool one = np == 1;
-    switch (grad.type) {
-    case MPZCH_F32: TRY(launch_reduce<float, STEP>(a, width, one, grid, s)); break;
-    case MPZCH_BF16: TRY(launch_reduce<__bf16, STEP>(a, width, one, grid, s)); break;
-    default: TRY(launch_reduce<_Float16, STEP>(a, width, one, grid, s)); break;
-    }
-    if (tiles > 1) {
-        a.lanes = grad.dim < kBlock ? pow2_at_least(grad.dim) : kBlock;
-        a.col_blocks = (int32_t)ceil_div(grad.dim, (int64_t)a.lanes * kJoinColumns);
-        TRY(launch(k_join<STEP>, tiles * a.col_blocks, kBlock, s, a, tiles));
-    }
-    return MPZCH_OK;
 }
 
 constexpr int64_t kMaxGradRows = ((int64_t)1 << 32) - 2;     // rows and the padding behind them in 32 bits, one value to spare

@@ -1,0 +1,442 @@
+// Sums over the sorted entries of a batch, for the gradient (MPZCH_TABLE_BYTES 0) or the step of a table whose elements have that
+// many bytes.
+#include "mpzch_host.hpp"
+#include "mpzch_reduce.hpp"
+
+namespace mpzch {
+
+namespace {
+
+// A run is the entries of one row.  A workgroup has a tile of neighbouring entries, a group of lanes in it (a power of two of
+// them, V * NP elements of the row for each) a part of the tile.  What a group knows of a run:
+//   it begins and ends in the part   the group emits its sum
+//   it began before                  the part's share goes to LDS, and whether the run goes on behind the part
+//   it goes on behind                the group in whose part it begins adds the following groups' shares, in their order
+// A run that goes on behind the tile for kBehind entries at most is finished there by the group that has its sum, and the
+// following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to write one is
+// found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and the run's
+// place alone determine: who is last does not change it.
+constexpr int kBehind = 32;
+constexpr uint32_t kNoRow = ~0u;
+constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part, and of a tile in LDS
+
+// elements of a table's row as they lie in memory, 16 or 32 bits each, so that they can be under way while others are added up
+template <int BYTES, int V>
+struct Raw {
+    typedef std::conditional_t<BYTES == 4, float, uint16_t> E;
+    Pack<E, V> v;
+    __device__ __forceinline__ void load(const char *rows, int64_t element) { v = *reinterpret_cast<const Pack<E, V> *>(rows + element * BYTES); }
+    __device__ __forceinline__ Floats<V> floats(int type) const
+    {
+        if constexpr (BYTES == 4) {
+            return __builtin_convertvector(v, Floats<V>);
+        } else {
+            typedef uint16_t u16v __attribute__((ext_vector_type(V)));
+            typedef __bf16 bf16v __attribute__((ext_vector_type(V)));
+            typedef _Float16 f16v __attribute__((ext_vector_type(V)));
+            const u16v bits = v;
+            return type == kBf16 ? __builtin_convertvector(__builtin_bit_cast(bf16v, bits), Floats<V>)
+                                 : __builtin_convertvector(__builtin_bit_cast(f16v, bits), Floats<V>);
+        }
+    }
+};
+
+// Shares are read by a workgroup that may run on another die, with an L2 of its own: they are stored and loaded as atomics of the
+// whole device, which go past the L2s one by one.  (A fence of the device instead writes the whole L2 back, the other workgroups'
+// outputs with it.)
+template <typename T>
+__device__ __forceinline__ void store_shared(T *to, T v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ __forceinline__ T load_shared(const T *at) { return __hip_atomic_load(const_cast<T *>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// this lane's stores have reached the memory that all dies see
+__device__ __forceinline__ void wait_for_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// how many of x(0) .. x(count - 1), ascending, are below v (or, with EQUAL, not above it): a wavefront looks at 64 of them at a time
+template <bool EQUAL, typename X>
+__device__ __forceinline__ int32_t wave_search(int32_t count, uint32_t v, X x)
+{
+    int32_t low = 0, high = count;               // the answer is in [low, high]
+    while (low < high) {
+        const int32_t step = (high - low + kWave - 1) / kWave;
+        const int32_t at = low + lane_id() * step;
+        bool below = false;
+        if (at < high) below = EQUAL ? x(at) <= v : x(at) < v;
+        const int yes = __popcll(__ballot(below));      // ascending: the first `yes` lanes
+        if (yes == 0) return low;
+        const int32_t last = low + (yes - 1) * step;
+        high = last + step < high ? last + step : high;
+        low = last + 1;
+    }
+    return low;
+}
+
+// The sum of a run whose shares lie in the tiles owner .. last, by a whole workgroup: `lanes` lanes (a power of two) for the
+// columns of this block, and the rest of it for every sharers-th tile.
+template <bool STEP>
+__device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint32_t row, int32_t owner, int32_t last, int32_t col_first,
+                                         int32_t col_end)
+{
+    constexpr int kColumns = 4;                  // of a lane at a time; a step has the whole row at once
+    int32_t lanes = kWave;
+    while (lanes < kBlock && lanes < col_end - col_first) lanes *= 2;
+    const int sharers = kBlock / lanes, sharer = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    const int64_t index = STEP ? 0 : load_shared(a.tail_index + owner);
+    for (int32_t c0 = col_first; c0 < col_end; c0 += kColumns * lanes) {
+        float sum[kColumns];
+        float squares = 0.f;
+#pragma unroll
+        for (int p = 0; p < kColumns; ++p) {
+            const int32_t c = c0 + p * lanes + lane;
+            sum[p] = 0.f;
+            if (c < col_end) {
+                if (sharer == 0) sum[p] = load_shared(a.tail + (int64_t)owner * a.dim + c);
+#pragma unroll 8
+                for (int32_t t = owner + 1 + sharer; t <= last; t += sharers) sum[p] += load_shared(a.head + (int64_t)t * a.dim + c);
+            }
+            if (sharers > 1) {
+                part[threadIdx.x] = sum[p];
+                __syncthreads();
+                if (sharer == 0)
+                    for (int g = 1; g < sharers; ++g) sum[p] += part[g * lanes + lane];
+                __syncthreads();
+            }
+            sum[p] *= a.factor;
+            if (c < col_end && sharer == 0) squares += sum[p] * sum[p];
+        }
+        if constexpr (STEP) {
+            const float lr = *a.lr;
+            float rate = lr;
+            if (a.state) {
+                part[threadIdx.x] = squares;
+                __syncthreads();
+                for (int d = kBlock / 2; d > 0; d >>= 1) {
+                    if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
+                    __syncthreads();
+                }
+                const float state = a.state[row] + part[0] / (float)a.dim;
+                __syncthreads();                  // (all have read it)
+                if (threadIdx.x == 0) a.state[row] = state;
+                rate = lr / (sqrtf(state) + a.eps);
+            }
+#pragma unroll
+            for (int p = 0; p < kColumns; ++p) {
+                const int32_t c = c0 + p * lanes + lane;
+                if (c >= col_end || sharer != 0) continue;
+                const int64_t element = (int64_t)row * a.row_stride + c;
+                store_typed<1>(a.type, a.rows, element, load_typed<1>(a.type, a.rows, element) - sum[p] * rate);
+            }
+        } else if (sharer == 0 && index < a.cap) {
+            if (c0 == 0 && lane == 0) a.out_slots[index] = row;
+#pragma unroll
+            for (int p = 0; p < kColumns; ++p) {
+                const int32_t c = c0 + p * lanes + lane;
+                if (c < col_end) store_typed<1>(a.type, a.out_rows, index * a.dim + c, Floats<1>(sum[p]));
+            }
+        }
+    }
+}
+
+// WB: bytes of an element of the table, for a step; 0: the gradient
+template <typename TG, int V, int NP, int WB>
+__global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
+{
+    constexpr bool STEP = WB != 0;
+    __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
+    __shared__ uint32_t sums[kWavesPerBlock], part_heads[kBlock], part_flags[kBlock], tile_shares;
+    __shared__ Floats<V> shares[NP][kBlock];
+
+    const int32_t tile_index = (int32_t)(blockIdx.x / (uint32_t)a.col_blocks), block_col = (int32_t)(blockIdx.x % (uint32_t)a.col_blocks);
+    const int64_t first = (int64_t)tile_index * a.tile;
+    const int64_t left = a.n - first;
+    const int m = (int)(left < a.tile ? left : a.tile);
+    const int behind = (int)(left - m < kBehind ? left - m : kBehind);
+    const int groups = kBlock / a.lanes, per = a.tile / groups;
+    const int group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
+
+    // the tile's entries and the next ones, the row before them and the one behind
+    for (int k = threadIdx.x; k < m + behind; k += kBlock) {
+        const uint64_t e = a.entries[first + k];
+        row_of_entry[k + 1] = (uint32_t)(e >> 32);
+        position[k] = (uint32_t)e;
+    }
+    if (threadIdx.x == 0) {
+        row_of_entry[0] = first > 0 ? row_at(a.entries, first - 1) : kNoRow;
+        row_of_entry[m + behind + 1] = first + m + behind < a.n ? row_at(a.entries, first + m + behind) : kNoRow;
+        tile_shares = 0;
+    }
+    // runs before the tile
+    uint32_t index = 0;
+    if constexpr (!STEP) {
+        if (a.heads_are == kBeforeTile) {
+            index = a.heads[tile_index];
+        } else {
+            uint32_t mine = 0;
+            if (a.heads_are == kOfTile)
+                for (int t = threadIdx.x; t < tile_index; t += kBlock) mine += a.heads[t];
+            else
+#pragma unroll 4
+                for (int64_t i = threadIdx.x; i < first; i += kBlock) {
+                    const uint32_t row = row_at(a.entries, i);
+                    mine += row != a.num_rows && (i == 0 || row_at(a.entries, i - 1) != row);
+                }
+            block_prefix(mine, sums, &index);
+        }
+    }
+    part_heads[threadIdx.x] = 0;
+    __syncthreads();
+    const int begin = group * per < m ? group * per : m, end = begin + per < m ? begin + per : m;
+    if constexpr (!STEP) {
+        uint32_t mine = 0;
+        for (int k = begin + lane; k < end; k += a.lanes)
+            mine += row_of_entry[k + 1] != a.num_rows && row_of_entry[k + 1] != row_of_entry[k];
+        for (int d = 1; d < a.lanes; d <<= 1) mine += __shfl_xor(mine, d);
+        if (lane == 0) part_heads[group] = mine;
+        __syncthreads();
+        uint32_t all;
+        const uint32_t before = block_prefix(part_heads[threadIdx.x], sums, &all);
+        part_heads[threadIdx.x] = before;
+        __syncthreads();
+        if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *a.out_count = (int64_t)index + all;
+        index += part_heads[group];
+    }
+    // what is left out: padding, and the rest of a run that an earlier tile has finished
+    const uint32_t tile_end_row = m > 0 ? row_of_entry[m] : kNoRow;
+    const bool begins_inside = m > 0 && row_of_entry[0] == row_of_entry[1];
+    // (the entry kBehind behind the tile's begin; it is in LDS, for the tile and kBehind more are)
+    const bool finished = begins_inside && row_of_entry[1 + (kBehind < m + behind ? kBehind : m + behind)] != row_of_entry[1];
+    const uint32_t skipped = finished ? row_of_entry[1] : a.num_rows;
+    const bool leaves = m > 0 && row_of_entry[m + 1] == tile_end_row && tile_end_row != a.num_rows && tile_end_row != skipped;
+    const bool long_run = leaves && row_of_entry[m + behind + 1] == tile_end_row;      // further than kBehind behind the tile
+
+    int32_t column[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) column[p] = ((block_col * NP + p) * a.lanes + lane) * V;
+    const uint64_t seed = a.mask.threshold ? *a.mask.seed : 0;
+    const float lr = STEP ? *a.lr : 0.f;
+    Floats<V> sum[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) sum[p] = Floats<V>(0.f);
+
+    typedef Raw<STEP ? WB : 4, V> Weights;
+    auto load_weights = [&](uint32_t row, Weights (&w)[NP], float &state) {
+        state = a.state ? a.state[row] : 0.f;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            if (column[p] < a.dim) w[p].load(a.rows, (int64_t)row * a.row_stride + column[p]);
+    };
+    // a finished sum
+    auto emit_step = [&](uint32_t row, const Weights (&w)[NP], float state) {
+        float rate = lr;
+        if (a.state) {
+            float squares = 0.f;
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float g = sum[p][e] * a.factor;
+                    if (column[p] < a.dim) squares += g * g;
+                }
+            for (int d = 1; d < a.lanes; d <<= 1) squares += __shfl_xor(squares, d);
+            state += squares / (float)a.dim;
+            if (lane == 0) a.state[row] = state;
+            rate = lr / (sqrtf(state) + a.eps);
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            if (column[p] < a.dim)
+                store_typed<V>(a.type, a.rows, (int64_t)row * a.row_stride + column[p], w[p].floats(a.type) - sum[p] * a.factor * rate);
+    };
+    auto emit_grad = [&](uint32_t row, uint32_t at) {
+        if ((int64_t)at >= a.cap) return;
+        if (block_col == 0 && lane == 0) a.out_slots[at] = row;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor);
+    };
+    auto load_grad = [&](uint32_t at, bool wanted, Floats<V> (&g)[NP]) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            g[p] = Floats<V>(0.f);
+            if (wanted && column[p] < a.dim)
+                g[p] = load_floats<TG, V>(a.grad + (int64_t)at * a.grad_stride + (int64_t)column[p] * sizeof(TG));
+        }
+    };
+    auto add = [&](const Floats<V> (&g)[NP], uint32_t at) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) sum[p] += a.mask.threshold ? masked<V>(g[p], seed, a.mask, at, column[p]) : g[p];
+    };
+
+    constexpr int kAhead = NP * V > 16 ? 2 : 4;
+    uint32_t flags = 0;
+    bool from_before = begin < end && row_of_entry[begin] == row_of_entry[begin + 1];
+    for (int k0 = begin; k0 < end; k0 += kAhead) {
+        Floats<V> g[kAhead][NP];
+        Weights w[kAhead][NP];
+        float state[kAhead];
+        uint32_t at[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = k0 + u < end ? k0 + u : end - 1;
+            const uint32_t row = row_of_entry[k + 1];
+            const bool wanted = k0 + u < end && row != a.num_rows && row != skipped;
+            at[u] = position[k];
+            load_grad(at[u], wanted, g[u]);
+            if constexpr (STEP)
+                if (wanted && row_of_entry[k + 2] != row) load_weights(row, w[u], state[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = k0 + u;
+            if (k >= end) break;
+            const uint32_t row = row_of_entry[k + 1];
+            if (row == a.num_rows || row == skipped) {
+                from_before = false;
+                continue;
+            }
+            if (row_of_entry[k] != row) ++index;
+            add(g[u], at[u]);
+            const bool goes_on = row_of_entry[k + 2] == row;
+            if (goes_on && k + 1 < end) continue;
+            if (from_before) {
+                flags |= kHeadShare | (goes_on ? kThrough : 0);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) shares[p][threadIdx.x] = sum[p];
+            } else if (goes_on) {
+                flags |= kTailShare;
+            } else if constexpr (STEP) {
+                emit_step(row, w[u], state[u]);
+            } else {
+                emit_grad(row, index - 1);
+            }
+            from_before = false;
+            if (!goes_on) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) sum[p] = Floats<V>(0.f);
+            }
+        }
+    }
+    if (lane == 0) part_flags[group] = flags;
+    __syncthreads();
+
+    // The run that the part leaves unfinished, and (first group) the one that came from the tile before.
+    for (int which = 0; which < 2; ++which) {
+        const bool tail = which == 0;
+        if (tail ? !(flags & kTailShare) : group != 0 || !(part_flags[0] & kHeadShare)) continue;
+        const uint32_t row = row_of_entry[tail ? end : 1];
+        int g = group + 1;
+        if (!tail) {
+            g = 0;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) sum[p] = Floats<V>(0.f);
+        }
+        bool goes_on = true;                     // shares of the parts from g on, as far as the run goes
+        for (; g < groups && goes_on; ++g) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) sum[p] += shares[p][g * a.lanes + lane];
+            goes_on = part_flags[g] & kThrough;
+        }
+        if (goes_on && !long_run) {              // the entries behind the tile
+            for (int k0 = m; row_of_entry[k0 + 1] == row; k0 += kAhead) {
+                Floats<V> v[kAhead][NP];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const int k = k0 + u < m + behind ? k0 + u : m + behind - 1;
+                    load_grad(position[k], k0 + u < m + behind && row_of_entry[k + 1] == row, v[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const int k = k0 + u < m + behind ? k0 + u : m + behind - 1;
+                    add(v[u], position[k]);      // (zeros where the run has ended)
+                }
+                if (k0 + kAhead >= m + behind) break;
+            }
+        }
+        if (tail && !(goes_on && long_run)) {
+            if constexpr (STEP) {
+                Weights w[NP];
+                float state;
+                load_weights(row, w, state);
+                emit_step(row, w, state);
+            } else {
+                emit_grad(row, index - 1);
+            }
+            continue;
+        }
+        float *to = (tail ? a.tail : a.head) + (int64_t)tile_index * a.dim;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            if (column[p] >= a.dim) continue;
+#pragma unroll
+            for (int e = 0; e < V; ++e) store_shared(to + column[p] + e, sum[p][e]);
+        }
+        if (lane == 0) {
+            if (tail && block_col == 0) store_shared(a.tail_index + tile_index, index - 1);
+            atomicOr(&tile_shares, tail ? kTailShare : kHeadShare);
+        }
+    }
+    wait_for_stores();
+    __syncthreads();
+    const uint32_t written = tile_shares;
+    if (!written) return;
+
+    // The shares are in memory before the counter says so, and the last workgroup of a run reads them behind it.
+    float *const part = reinterpret_cast<float *>(&shares[0][0]);
+    const int32_t col_first = block_col * NP * V * a.lanes;
+    const int32_t col_end = col_first + NP * V * a.lanes < a.dim ? col_first + NP * V * a.lanes : a.dim;
+    for (uint32_t share = kHeadShare; share <= kTailShare; share <<= 2) {
+        if (!(written & share)) continue;        // (the same for the whole workgroup)
+        const uint32_t row = share == kHeadShare ? row_of_entry[1] : tile_end_row;
+        // the tile in which the run begins, and the last one that it goes into by more than kBehind entries
+        int32_t owner = tile_index;
+        if (share == kHeadShare) {
+            owner = wave_search<false>(a.tiles, row, [&](int32_t t) { return row_at(a.entries, (int64_t)t * a.tile); });
+            if (owner > 0 && row_at(a.entries, (int64_t)owner * a.tile - 1) == row) --owner;       // (it begins at a tile's begin, or inside one)
+        }
+        const int32_t last = wave_search<true>(a.tiles, row, [&](int32_t t) {
+            const int64_t i = (int64_t)t * a.tile + kBehind;
+            return i < a.n ? row_at(a.entries, i) : kNoRow;
+        }) - 1;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint32_t *counter = a.arrived + (int64_t)owner * a.col_blocks + block_col;
+            const bool is_last = atomicAdd(counter, 1u) == (uint32_t)(last - owner);
+            if (is_last) store_shared(counter, 0u);
+            tile_shares = is_last;
+        }
+        __syncthreads();
+        if (!tile_shares) continue;
+        join_run<STEP>(a, part, row, owner, last, col_first, col_end);
+        __syncthreads();
+    }
+}
+
+template <typename TG, int WB>
+mpzch_status_t launch_reduce(const ReduceArgs &a, int width, int pieces, int grid, hipStream_t s)
+{
+    switch (width) {
+    case 8:
+        if constexpr (sizeof(TG) == 2)
+            return pieces == 1 ? launch(k_reduce<TG, 8, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 8, 2, WB>, grid, kBlock, s, a);
+        return MPZCH_ERR_UNSUPPORTED;
+    case 4: return pieces == 1 ? launch(k_reduce<TG, 4, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 4, 4, WB>, grid, kBlock, s, a);
+    case 2: return pieces == 1 ? launch(k_reduce<TG, 2, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 2, 8, WB>, grid, kBlock, s, a);
+    default: return pieces == 1 ? launch(k_reduce<TG, 1, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 1, 16, WB>, grid, kBlock, s, a);
+    }
+}
+template <int WB>
+mpzch_status_t launch_reduce(const ReduceArgs &a, int32_t grad_type, int width, int pieces, int grid, hipStream_t s)
+{
+    switch (grad_type) {
+    case MPZCH_F32: return launch_reduce<float, WB>(a, width, pieces, grid, s);
+    case MPZCH_BF16: return launch_reduce<__bf16, WB>(a, width, pieces, grid, s);
+    default: return launch_reduce<_Float16, WB>(a, width, pieces, grid, s);
+    }
+}
+
+}  // namespace
+
+#define MPZCH_DEFINE(bytes) MPZCH_LAUNCH_REDUCE(bytes) { return launch_reduce<bytes>(a, grad_type, width, pieces, grid, s); }
+#define MPZCH_DEFINE_FOR(bytes) MPZCH_DEFINE(bytes)
+MPZCH_DEFINE_FOR(MPZCH_TABLE_BYTES)
+
+}  // namespace mpzch

@@ -1,0 +1,269 @@
+// Sort of a batch's slots by row.
+#pragma once
+#include "mpzch_embed_kernels.hpp"
+
+namespace mpzch {
+
+constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / kWave;
+
+// Entries {row << 32 | position} in ascending order.  Padding has the row num_rows and ends up behind everything.
+struct SortSource {
+    const int64_t *slots;        // first pass: entries are made from them
+    const uint64_t *entries;     // later ones
+    RowMod mod;
+    int64_t n;
+    int32_t shift, bits;         // of the digit inside an entry
+};
+__device__ __forceinline__ uint32_t sort_row(const RowMod &mod, int64_t slot)
+{
+    return slot < 0 ? (uint32_t)mod.num_rows : (uint32_t)row_of(mod, slot);
+}
+template <bool FIRST>
+__device__ __forceinline__ uint64_t sort_entry(const SortSource &s, int64_t i)
+{
+    if constexpr (FIRST) return (uint64_t)sort_row(s.mod, s.slots[i]) << 32 | (uint64_t)i;
+    else return s.entries[i];
+}
+
+// Short batches: an entry's place is the number of entries before it, counted over all of them by 64 lanes with an entry each
+// and 16 wavefronts with a part of the batch each.  n^2 comparisons, but one launch.
+constexpr int kRankMax = 8192;
+__global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, RowMod mod, int32_t n, uint64_t *out)
+{
+    __shared__ __align__(16) uint32_t rows[kRankMax];
+    __shared__ uint32_t place[kWave];
+    const int32_t whole = (n + 3) / 4 * 4;
+    for (int32_t i = threadIdx.x; i < whole; i += kSortBlock) rows[i] = i < n ? sort_row(mod, slots[i]) : ~0u;
+    if (threadIdx.x < kWave) place[threadIdx.x] = 0;
+    __syncthreads();
+    const int32_t block = (int32_t)blockIdx.x * kWave, mine = block + lane_id();
+    const uint32_t row = rows[mine < n ? mine : n - 1];
+    const int32_t wave = threadIdx.x / kWave, share = (whole / 4 + kSortWaves - 1) / kSortWaves * 4;
+    const int32_t begin = wave * share < whole ? wave * share : whole, end = begin + share < whole ? begin + share : whole;
+    uint32_t before = 0;
+    auto upto = [&](int32_t at, int32_t from, int32_t to) { return at < from ? from : at > to ? to : at; };
+    // entries before the 64 of this workgroup, among them, behind them
+    const int32_t first = upto(block, begin, end), last = upto(block + kWave, begin, end);
+#pragma unroll 4
+    for (int32_t j = begin; j < first; j += 4) {
+        const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
+        before += (r[0] <= row) + (r[1] <= row) + (r[2] <= row) + (r[3] <= row);
+    }
+    for (int32_t j = first; j < last; ++j) before += rows[j] < row || (rows[j] == row && j < mine);
+#pragma unroll 4
+    for (int32_t j = last; j < end; j += 4) {
+        const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
+        before += (r[0] < row) + (r[1] < row) + (r[2] < row) + (r[3] < row);
+    }
+    atomicAdd(&place[lane_id()], before);
+    __syncthreads();
+    if (threadIdx.x < kWave && mine < n) out[place[threadIdx.x]] = (uint64_t)row << 32 | (uint32_t)mine;
+}
+
+// Longer ones: a radix sort, least significant digit first, each pass stable, so that the positions of a row stay ascending.
+// A pass counts the digits of every tile (k_sort_hist), adds up what earlier tiles hold (k_sort_scan; where there are few
+// tiles, k_sort_scatter itself) and moves the entries (k_sort_scatter).
+constexpr int kMaxDigitBits = 11, kMaxDigits = 1 << kMaxDigitBits;
+
+// hist[tile][digit]: how many entries of the tile have the digit, 16 bits each
+template <bool FIRST, int ITEMS>
+__global__ __launch_bounds__(kSortBlock) void k_sort_hist(SortSource s, uint32_t *hist)
+{
+    __shared__ uint32_t count[kMaxDigits];
+    const uint32_t digits = 1u << s.bits;
+    for (uint32_t d = threadIdx.x; d < digits; d += kSortBlock) count[d] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * (kSortBlock * ITEMS);
+    uint64_t entry[ITEMS];
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const int64_t i = first + u * kSortBlock + threadIdx.x;
+        entry[u] = i < s.n ? sort_entry<FIRST>(s, i) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u)
+        if (first + u * kSortBlock + threadIdx.x < s.n) atomicAdd(&count[(uint32_t)(entry[u] >> s.shift) & (digits - 1)], 1u);
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < digits / 2; d += kSortBlock)
+        hist[(int64_t)blockIdx.x * (digits / 2) + d] = count[2 * d] | count[2 * d + 1] << 16;
+}
+
+// before[tile][digit]: entries of earlier tiles with the digit; behind the last tile the entries of all.  A workgroup has 64 digits,
+// each lane two of them and a 32nd of the tiles.
+constexpr int kScanDigits = 64;
+__global__ __launch_bounds__(kSortBlock) void k_sort_scan(const uint32_t *hist, uint32_t *before, int32_t tiles, int32_t bits)
+{
+    __shared__ uint32_t low[32][32], high[32][32];
+    const int32_t pairs = 1 << (bits - 1);
+    const int32_t pair = (int32_t)blockIdx.x * (kScanDigits / 2) + (int32_t)(threadIdx.x & 31), part = threadIdx.x / 32;
+    const int32_t per = (tiles + 31) / 32, begin = part * per < tiles ? part * per : tiles, end = begin + per < tiles ? begin + per : tiles;
+    uint32_t a = 0, b = 0;
+#pragma unroll 8
+    for (int32_t t = begin; t < end; ++t) {
+        const uint32_t v = hist[(int64_t)t * pairs + pair];
+        a += v & 0xFFFF;
+        b += v >> 16;
+    }
+    low[part][threadIdx.x & 31] = a;
+    high[part][threadIdx.x & 31] = b;
+    __syncthreads();
+    a = b = 0;
+    for (int32_t q = 0; q < part; ++q) {
+        a += low[q][threadIdx.x & 31];
+        b += high[q][threadIdx.x & 31];
+    }
+    for (int32_t t = begin; t <= end; ++t) {
+        if (t == end && !(part == 31)) break;
+        uint32_t *to = before + ((int64_t)t * pairs + pair) * 2;
+        to[0] = a;
+        to[1] = b;
+        if (t == end) break;
+        const uint32_t v = hist[(int64_t)t * pairs + pair];
+        a += v & 0xFFFF;
+        b += v >> 16;
+    }
+}
+
+// Every wavefront ranks its entries 64 at a time: the lanes with the same digit find each other by ballots over the digit's
+// bits, the first of them adds their number to the wavefront's count in LDS (its own, so the order of its accesses is that of
+// the program).  The entries then go to LDS in their new order, so that neighbouring lanes store neighbouring entries.
+template <bool FIRST, int ITEMS>
+__global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const uint32_t *hist, const uint32_t *before, int32_t tiles,
+                                                              uint64_t *out)
+{
+    constexpr int kTile = kSortBlock * ITEMS;
+    // the counts of the wavefronts, 16 bits each, and then the entries
+    constexpr int kCountBytes = kSortWaves * kMaxDigits * 2, kEntryBytes = kTile * 8;
+    __shared__ __align__(16) unsigned char area[kCountBytes > kEntryBytes ? kCountBytes : kEntryBytes];
+    __shared__ uint16_t local[kMaxDigits];         // (two workgroups on a compute unit)
+    __shared__ uint32_t global[kMaxDigits], sums[kSortWaves];
+    uint16_t *const count = reinterpret_cast<uint16_t *>(area);
+    uint64_t *const sorted = reinterpret_cast<uint64_t *>(area);
+    const uint32_t digits = 1u << s.bits, pairs = digits / 2;
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    for (uint32_t k = threadIdx.x; k < kSortWaves * pairs / 4; k += kSortBlock) reinterpret_cast<u32x4 *>(area)[k] = u32x4(0);
+    const int64_t first = (int64_t)blockIdx.x * kTile;
+    const int64_t left = s.n - first;
+    const int mine = (int)(left < kTile ? left : kTile);
+    uint64_t entry[ITEMS];
+    uint32_t place[ITEMS];
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const int at = wave * (kWave * ITEMS) + u * kWave + lane;
+        entry[u] = at < mine ? sort_entry<FIRST>(s, first + at) : 0;
+    }
+    // what earlier tiles hold of this lane's two digits, and all tiles
+    uint32_t earlier[2] = {0, 0}, all[2] = {0, 0};
+    if (threadIdx.x < pairs) {
+        if (before) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                earlier[k] = before[((int64_t)blockIdx.x * pairs + threadIdx.x) * 2 + k];
+                all[k] = before[((int64_t)tiles * pairs + threadIdx.x) * 2 + k];
+            }
+        } else {
+#pragma unroll 8
+            for (int32_t t = 0; t < tiles; ++t) {
+                const uint32_t v = hist[(int64_t)t * pairs + threadIdx.x];
+                const uint32_t early = t < (int32_t)blockIdx.x ? v : 0;
+                earlier[0] += early & 0xFFFF;
+                earlier[1] += early >> 16;
+                all[0] += v & 0xFFFF;
+                all[1] += v >> 16;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const bool there = wave * (kWave * ITEMS) + u * kWave + lane < mine;
+        const uint32_t digit = (uint32_t)(entry[u] >> s.shift) & (digits - 1);
+        uint64_t same = __ballot(there);
+        for (int b = 0; b < s.bits; ++b) {
+            const uint64_t set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        const uint32_t at = (uint32_t)wave * digits + digit;
+        const uint32_t so_far = count[at];
+        place[u] = so_far + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        __builtin_amdgcn_wave_barrier();
+        if (there && (same >> lane) == 1) count[at] = (uint16_t)(place[u] + 1);       // the last of them
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    {
+        // counts of earlier wavefronts, two digits in a word (no carry: a tile has less than 2^16 entries)
+        uint32_t sum = 0;
+        if (threadIdx.x < pairs) {
+            uint32_t c[kSortWaves];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) c[w] = reinterpret_cast<uint32_t *>(area)[w * pairs + threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                reinterpret_cast<uint32_t *>(area)[w * pairs + threadIdx.x] = sum;
+                sum += c[w];
+            }
+        }
+        uint32_t total;
+        const uint32_t here = block_prefix((sum & 0xFFFF) + (sum >> 16), sums, &total);
+        const uint32_t there = block_prefix(all[0] + all[1], sums, &total);
+        if (threadIdx.x < pairs) {
+            local[2 * threadIdx.x] = (uint16_t)here;
+            local[2 * threadIdx.x + 1] = (uint16_t)(here + (sum & 0xFFFF));
+            global[2 * threadIdx.x] = there + earlier[0] - here;
+            global[2 * threadIdx.x + 1] = there + all[0] + earlier[1] - here - (sum & 0xFFFF);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const uint32_t digit = (uint32_t)(entry[u] >> s.shift) & (digits - 1);
+        place[u] += local[digit] + count[(uint32_t)wave * digits + digit];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u)
+        if (wave * (kWave * ITEMS) + u * kWave + lane < mine) sorted[place[u]] = entry[u];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+        const int at = u * kSortBlock + threadIdx.x;
+        if (at >= mine) continue;
+        const uint64_t e = sorted[at];
+        out[global[(uint32_t)(e >> s.shift) & (digits - 1)] + (uint32_t)at] = e;       // (the sum is below n; the parts may wrap)
+    }
+}
+
+// runs that begin in each tile
+__global__ __launch_bounds__(kBlock) void k_count_heads(const uint64_t *entries, int64_t n, uint32_t num_rows, int32_t tile,
+                                                         uint32_t *heads)
+{
+    __shared__ uint32_t sums[kWavesPerBlock];
+    const int64_t first = (int64_t)blockIdx.x * tile;
+    uint32_t mine = 0;
+    for (int k = threadIdx.x; k < tile; k += kBlock) {
+        const int64_t i = first + k;
+        if (i >= n) break;
+        const uint32_t row = row_at(entries, i);
+        mine += row != num_rows && (i == 0 || row_at(entries, i - 1) != row);
+    }
+    uint32_t total;
+    block_prefix(mine, sums, &total);
+    if (threadIdx.x == 0) heads[blockIdx.x] = total;
+}
+// heads of tiles -> heads of all tiles before, in place; one workgroup
+__global__ __launch_bounds__(kSortBlock) void k_scan_heads(uint32_t *heads, int32_t tiles)
+{
+    __shared__ uint32_t sums[kSortWaves];
+    uint32_t carry = 0;
+    for (int32_t t0 = 0; t0 < tiles; t0 += kSortBlock) {
+        const int32_t t = t0 + (int32_t)threadIdx.x;
+        const uint32_t v = t < tiles ? heads[t] : 0;
+        uint32_t total;
+        const uint32_t before = block_prefix(v, sums, &total);
+        if (t < tiles) heads[t] = carry + before;
+        carry += total;
+    }
+}
+
+}  // namespace mpzch
