@@ -110,7 +110,7 @@ ReducePlan reduce_plan(int64_t n, int64_t dim, int width)
     p.lanes = pieces < kWave ? pow2_at_least(pieces) : kWave;
     p.pieces = pieces <= kWave ? 1 : many_pieces(width);
     p.col_blocks = (int)ceil_div(pieces, (int64_t)p.lanes * p.pieces);
-    const int groups = kBlock / p.lanes;
+    const int groups = kReduceBlock / p.lanes;
     int64_t per = ceil_div(n * p.lanes * p.col_blocks, kWave * kReduceWaves);
     if (per < kPartMin) per = kPartMin;
     if (per > kReduceTile / groups) per = kReduceTile / groups;
@@ -119,10 +119,11 @@ ReducePlan reduce_plan(int64_t n, int64_t dim, int width)
     return p;
 }
 // most tiles, and most columns' blocks, of any batch of up to n positions and rows of up to dim elements: the parts are as
-// short as the number of wavefronts allows (kReduceWaves / kWavesPerBlock tiles), or the tiles as long as can be
+// short as the number of wavefronts allows (kReduceWaves wavefronts in all), or the tiles as long as can be
 int64_t most_tiles(int64_t n)
 {
-    const int64_t some = ceil_div(n, 4 * kPartMin) < kReduceWaves / kWavesPerBlock ? ceil_div(n, 4 * kPartMin) : kReduceWaves / kWavesPerBlock;
+    const int64_t waves = kReduceBlock / kWave;
+    const int64_t some = ceil_div(n, waves * kPartMin) < kReduceWaves / waves ? ceil_div(n, waves * kPartMin) : kReduceWaves / waves;
     const int64_t full = ceil_div(n, kReduceTile);
     return 1 + (some > full ? some : full);
 }

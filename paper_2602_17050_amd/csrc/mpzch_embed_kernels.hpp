@@ -56,6 +56,27 @@ __device__ __forceinline__ void store_typed(int type, char *base, int64_t elemen
     else store_floats<_Float16, V>(base + element * 2, v);
 }
 
+// V elements as they lie in memory, 16 or 32 bits each: converted where they are used, so that many loads can be under way
+template <int BYTES, int V>
+struct Raw {
+    typedef std::conditional_t<BYTES == 4, float, uint16_t> E;
+    Pack<E, V> v;
+    __device__ __forceinline__ void load(const char *rows, int64_t element) { v = *reinterpret_cast<const Pack<E, V> *>(rows + element * BYTES); }
+    __device__ __forceinline__ Floats<V> floats(int type) const
+    {
+        if constexpr (BYTES == 4) {
+            return __builtin_convertvector(v, Floats<V>);
+        } else {
+            typedef uint16_t u16v __attribute__((ext_vector_type(V)));
+            typedef __bf16 bf16v __attribute__((ext_vector_type(V)));
+            typedef _Float16 f16v __attribute__((ext_vector_type(V)));
+            const u16v bits = v;
+            return type == kBf16 ? __builtin_convertvector(__builtin_bit_cast(bf16v, bits), Floats<V>)
+                                 : __builtin_convertvector(__builtin_bit_cast(f16v, bits), Floats<V>);
+        }
+    }
+};
+
 // ------------------------------------------------------------------ the mask
 constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
 
@@ -125,7 +146,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a)
     for (int64_t i = (int64_t)blockIdx.x * kBlock * kEmbedPieces + threadIdx.x; i - threadIdx.x < total; i += turn) {
         int64_t k[kEmbedPieces], slot[kEmbedPieces];
         uint32_t c[kEmbedPieces];
-        Floats<V> v[kEmbedPieces];
+        Raw<sizeof(TI), V> v[kEmbedPieces];
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
             k[u] = k0 + divided(a.pieces, c0 + u * kBlock + threadIdx.x, &c[u]);
@@ -133,14 +154,14 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a)
         }
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
-            v[u] = Floats<V>(0.f);
-            if (slot[u] >= 0)
-                v[u] = load_floats<TI, V>(a.rows + row_of(a.mod, slot[u]) * a.row_stride + (int64_t)c[u] * (V * sizeof(TI)));
+            // (padding: the first row, in the caches)
+            const int64_t row = slot[u] >= 0 ? row_of(a.mod, slot[u]) : 0;
+            v[u].load(a.rows + row * a.row_stride, c[u] * V);
         }
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
             if (i + u * kBlock >= total) continue;
-            Floats<V> x = v[u] * a.factor;
+            Floats<V> x = v[u].floats(std::is_same_v<TI, __bf16> ? kBf16 : kF16) * a.factor;
             if constexpr (DROP) x = masked<V>(x, seed, a.mask, k[u], (int32_t)(c[u] * V));
             if (slot[u] < 0) x = Floats<V>(0.f);
             store_floats<TO, V>(a.out + k[u] * a.out_stride + (int64_t)c[u] * (V * sizeof(TO)), x);

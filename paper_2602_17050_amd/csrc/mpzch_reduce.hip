@@ -20,27 +20,6 @@ constexpr int kBehind = 32;
 constexpr uint32_t kNoRow = ~0u;
 constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part, and of a tile in LDS
 
-// elements of a table's row as they lie in memory, 16 or 32 bits each, so that they can be under way while others are added up
-template <int BYTES, int V>
-struct Raw {
-    typedef std::conditional_t<BYTES == 4, float, uint16_t> E;
-    Pack<E, V> v;
-    __device__ __forceinline__ void load(const char *rows, int64_t element) { v = *reinterpret_cast<const Pack<E, V> *>(rows + element * BYTES); }
-    __device__ __forceinline__ Floats<V> floats(int type) const
-    {
-        if constexpr (BYTES == 4) {
-            return __builtin_convertvector(v, Floats<V>);
-        } else {
-            typedef uint16_t u16v __attribute__((ext_vector_type(V)));
-            typedef __bf16 bf16v __attribute__((ext_vector_type(V)));
-            typedef _Float16 f16v __attribute__((ext_vector_type(V)));
-            const u16v bits = v;
-            return type == kBf16 ? __builtin_convertvector(__builtin_bit_cast(bf16v, bits), Floats<V>)
-                                 : __builtin_convertvector(__builtin_bit_cast(f16v, bits), Floats<V>);
-        }
-    }
-};
-
 // Shares are read by a workgroup that may run on another die, with an L2 of its own: they are stored and loaded as atomics of the
 // whole device, which go past the L2s one by one.  (A fence of the device instead writes the whole L2 back, the other workgroups'
 // outputs with it.)
@@ -76,10 +55,12 @@ template <bool STEP>
 __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint32_t row, int32_t owner, int32_t last, int32_t col_first,
                                          int32_t col_end)
 {
-    constexpr int kColumns = 4;                  // of a lane at a time; a step has the whole row at once
+    constexpr int kColumns = 2;                  // of a lane at a time; a step has the whole row at once
+    constexpr int kJoinAhead = 8;
+    static_assert(!STEP || kColumns * kReduceBlock >= MPZCH_MAX_STEP_DIM);
     int32_t lanes = kWave;
-    while (lanes < kBlock && lanes < col_end - col_first) lanes *= 2;
-    const int sharers = kBlock / lanes, sharer = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    while (lanes < kReduceBlock && lanes < col_end - col_first) lanes *= 2;
+    const int sharers = kReduceBlock / lanes, sharer = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     const int64_t index = STEP ? 0 : load_shared(a.tail_index + owner);
     for (int32_t c0 = col_first; c0 < col_end; c0 += kColumns * lanes) {
         float sum[kColumns];
@@ -87,12 +68,27 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
 #pragma unroll
         for (int p = 0; p < kColumns; ++p) {
             const int32_t c = c0 + p * lanes + lane;
-            sum[p] = 0.f;
-            if (c < col_end) {
-                if (sharer == 0) sum[p] = load_shared(a.tail + (int64_t)owner * a.dim + c);
-#pragma unroll 8
-                for (int32_t t = owner + 1 + sharer; t <= last; t += sharers) sum[p] += load_shared(a.head + (int64_t)t * a.dim + c);
+            sum[p] = sharer == 0 && c < col_end ? load_shared(a.tail + (int64_t)owner * a.dim + c) : 0.f;
+        }
+        for (int32_t t0 = owner + 1 + sharer; t0 <= last; t0 += kJoinAhead * sharers) {
+            float v[kJoinAhead][kColumns];
+#pragma unroll
+            for (int u = 0; u < kJoinAhead; ++u) {
+                const int32_t t = t0 + u * sharers <= last ? t0 + u * sharers : last;
+#pragma unroll
+                for (int p = 0; p < kColumns; ++p) {
+                    const int32_t c = c0 + p * lanes + lane;
+                    v[u][p] = load_shared(a.head + (int64_t)t * a.dim + (c < col_end ? c : col_first));
+                }
             }
+#pragma unroll
+            for (int u = 0; u < kJoinAhead; ++u)
+#pragma unroll
+                for (int p = 0; p < kColumns; ++p) sum[p] += t0 + u * sharers <= last ? v[u][p] : 0.f;
+        }
+#pragma unroll
+        for (int p = 0; p < kColumns; ++p) {
+            const int32_t c = c0 + p * lanes + lane;
             if (sharers > 1) {
                 part[threadIdx.x] = sum[p];
                 __syncthreads();
@@ -109,7 +105,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
             if (a.state) {
                 part[threadIdx.x] = squares;
                 __syncthreads();
-                for (int d = kBlock / 2; d > 0; d >>= 1) {
+                for (int d = kReduceBlock / 2; d > 0; d >>= 1) {
                     if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
                     __syncthreads();
                 }
@@ -138,23 +134,23 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
 
 // WB: bytes of an element of the table, for a step; 0: the gradient
 template <typename TG, int V, int NP, int WB>
-__global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
+__global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 {
     constexpr bool STEP = WB != 0;
     __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
-    __shared__ uint32_t sums[kWavesPerBlock], part_heads[kBlock], part_flags[kBlock], tile_shares;
-    __shared__ Floats<V> shares[NP][kBlock];
+    __shared__ uint32_t sums[kReduceBlock / kWave], part_heads[kReduceBlock], part_flags[kReduceBlock], tile_shares;
+    __shared__ Floats<V> shares[NP][kReduceBlock];
 
     const int32_t tile_index = (int32_t)(blockIdx.x / (uint32_t)a.col_blocks), block_col = (int32_t)(blockIdx.x % (uint32_t)a.col_blocks);
     const int64_t first = (int64_t)tile_index * a.tile;
     const int64_t left = a.n - first;
     const int m = (int)(left < a.tile ? left : a.tile);
     const int behind = (int)(left - m < kBehind ? left - m : kBehind);
-    const int groups = kBlock / a.lanes, per = a.tile / groups;
+    const int groups = kReduceBlock / a.lanes, per = a.tile / groups;
     const int group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
 
     // the tile's entries and the next ones, the row before them and the one behind
-    for (int k = threadIdx.x; k < m + behind; k += kBlock) {
+    for (int k = threadIdx.x; k < m + behind; k += kReduceBlock) {
         const uint64_t e = a.entries[first + k];
         row_of_entry[k + 1] = (uint32_t)(e >> 32);
         position[k] = (uint32_t)e;
@@ -172,10 +168,10 @@ __global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
         } else {
             uint32_t mine = 0;
             if (a.heads_are == kOfTile)
-                for (int t = threadIdx.x; t < tile_index; t += kBlock) mine += a.heads[t];
+                for (int t = threadIdx.x; t < tile_index; t += kReduceBlock) mine += a.heads[t];
             else
 #pragma unroll 4
-                for (int64_t i = threadIdx.x; i < first; i += kBlock) {
+                for (int64_t i = threadIdx.x; i < first; i += kReduceBlock) {
                     const uint32_t row = row_at(a.entries, i);
                     mine += row != a.num_rows && (i == 0 || row_at(a.entries, i - 1) != row);
                 }
@@ -221,8 +217,7 @@ __global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
     auto load_weights = [&](uint32_t row, Weights (&w)[NP], float &state) {
         state = a.state ? a.state[row] : 0.f;
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-            if (column[p] < a.dim) w[p].load(a.rows, (int64_t)row * a.row_stride + column[p]);
+        for (int p = 0; p < NP; ++p) w[p].load(a.rows, (int64_t)row * a.row_stride + (column[p] < a.dim ? column[p] : 0));
     };
     // a finished sum
     auto emit_step = [&](uint32_t row, const Weights (&w)[NP], float state) {
@@ -253,24 +248,27 @@ __global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
         for (int p = 0; p < NP; ++p)
             if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor);
     };
-    auto load_grad = [&](uint32_t at, bool wanted, Floats<V> (&g)[NP]) {
+    // (unconditional loads, so that all that are asked for are under way at a time: where nothing is wanted, of a row that is in the
+    // caches anyway; a lane without columns has the first one)
+    typedef Raw<sizeof(TG), V> Gradient;
+    constexpr int kGradType = std::is_same_v<TG, float> ? kF32 : std::is_same_v<TG, __bf16> ? kBf16 : kF16;
+    auto load_grad = [&](uint32_t at, Gradient (&g)[NP]) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) g[p].load(a.grad + (int64_t)at * a.grad_stride, column[p] < a.dim ? column[p] : 0);
+    };
+    auto add = [&](const Gradient (&g)[NP], uint32_t at) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            g[p] = Floats<V>(0.f);
-            if (wanted && column[p] < a.dim)
-                g[p] = load_floats<TG, V>(a.grad + (int64_t)at * a.grad_stride + (int64_t)column[p] * sizeof(TG));
+            const Floats<V> v = g[p].floats(kGradType);
+            sum[p] += a.mask.threshold ? masked<V>(v, seed, a.mask, at, column[p]) : v;
         }
     };
-    auto add = [&](const Floats<V> (&g)[NP], uint32_t at) {
-#pragma unroll
-        for (int p = 0; p < NP; ++p) sum[p] += a.mask.threshold ? masked<V>(g[p], seed, a.mask, at, column[p]) : g[p];
-    };
 
-    constexpr int kAhead = NP * V > 16 ? 2 : 4;
+    constexpr int kAhead = NP >= 8 ? 2 : 4;
     uint32_t flags = 0;
     bool from_before = begin < end && row_of_entry[begin] == row_of_entry[begin + 1];
     for (int k0 = begin; k0 < end; k0 += kAhead) {
-        Floats<V> g[kAhead][NP];
+        Gradient g[kAhead][NP];
         Weights w[kAhead][NP];
         float state[kAhead];
         uint32_t at[kAhead];
@@ -278,11 +276,10 @@ __global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
         for (int u = 0; u < kAhead; ++u) {
             const int k = k0 + u < end ? k0 + u : end - 1;
             const uint32_t row = row_of_entry[k + 1];
-            const bool wanted = k0 + u < end && row != a.num_rows && row != skipped;
-            at[u] = position[k];
-            load_grad(at[u], wanted, g[u]);
-            if constexpr (STEP)
-                if (wanted && row_of_entry[k + 2] != row) load_weights(row, w[u], state[u]);
+            const bool wanted = row != a.num_rows && row != skipped;
+            at[u] = position[wanted ? k : 0];
+            load_grad(at[u], g[u]);
+            if constexpr (STEP) load_weights(wanted && row_of_entry[k + 2] != row ? row : 0, w[u], state[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -337,17 +334,16 @@ __global__ __launch_bounds__(kBlock) void k_reduce(ReduceArgs a)
         }
         if (goes_on && !long_run) {              // the entries behind the tile
             for (int k0 = m; row_of_entry[k0 + 1] == row; k0 += kAhead) {
-                Floats<V> v[kAhead][NP];
+                Gradient v[kAhead][NP];
+                uint32_t at[kAhead];
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    const int k = k0 + u < m + behind ? k0 + u : m + behind - 1;
-                    load_grad(position[k], k0 + u < m + behind && row_of_entry[k + 1] == row, v[u]);
+                    at[u] = position[k0 + u < m + behind ? k0 + u : m];
+                    load_grad(at[u], v[u]);
                 }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int k = k0 + u < m + behind ? k0 + u : m + behind - 1;
-                    add(v[u], position[k]);      // (zeros where the run has ended)
-                }
+                for (int u = 0; u < kAhead; ++u)
+                    if (k0 + u < m + behind && row_of_entry[k0 + u + 1] == row) add(v[u], at[u]);
                 if (k0 + kAhead >= m + behind) break;
             }
         }
@@ -416,11 +412,11 @@ mpzch_status_t launch_reduce(const ReduceArgs &a, int width, int pieces, int gri
     switch (width) {
     case 8:
         if constexpr (sizeof(TG) == 2)
-            return pieces == 1 ? launch(k_reduce<TG, 8, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 8, 2, WB>, grid, kBlock, s, a);
+            return pieces == 1 ? launch(k_reduce<TG, 8, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 8, 2, WB>, grid, kReduceBlock, s, a);
         return MPZCH_ERR_UNSUPPORTED;
-    case 4: return pieces == 1 ? launch(k_reduce<TG, 4, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 4, 4, WB>, grid, kBlock, s, a);
-    case 2: return pieces == 1 ? launch(k_reduce<TG, 2, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 2, 8, WB>, grid, kBlock, s, a);
-    default: return pieces == 1 ? launch(k_reduce<TG, 1, 1, WB>, grid, kBlock, s, a) : launch(k_reduce<TG, 1, 16, WB>, grid, kBlock, s, a);
+    case 4: return pieces == 1 ? launch(k_reduce<TG, 4, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 4, 4, WB>, grid, kReduceBlock, s, a);
+    case 2: return pieces == 1 ? launch(k_reduce<TG, 2, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 2, 8, WB>, grid, kReduceBlock, s, a);
+    default: return pieces == 1 ? launch(k_reduce<TG, 1, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 1, 16, WB>, grid, kReduceBlock, s, a);
     }
 }
 template <int WB>

@@ -5,6 +5,7 @@
 
 namespace mpzch {
 
+constexpr int kReduceBlock = 512;
 constexpr int kReduceTile = 2048;                // entries of a workgroup at most
 struct ReduceArgs {
     const uint64_t *entries;
