@@ -16,9 +16,9 @@ namespace {
 // following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to write one is
 // found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and the run's
 // place alone determine: who is last does not change it.
-constexpr int kBehind = 32;
+constexpr int kBehind = 128;
 constexpr uint32_t kNoRow = ~0u;
-constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part, and of a tile in LDS
+constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part
 
 // Shares are read by a workgroup that may run on another die, with an L2 of its own: they are stored and loaded as atomics of the
 // whole device, which go past the L2s one by one.  (A fence of the device instead writes the whole L2 back, the other workgroups'
@@ -65,6 +65,16 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
     for (int32_t c0 = col_first; c0 < col_end; c0 += kColumns * lanes) {
         float sum[kColumns];
         float squares = 0.f;
+        float weight[kColumns], state = 0.f, lr = 0.f;
+        if constexpr (STEP) {                    // (under way with the shares)
+            lr = *a.lr;
+            if (a.state) state = a.state[row];
+#pragma unroll
+            for (int p = 0; p < kColumns; ++p) {
+                const int32_t c = c0 + p * lanes + lane;
+                weight[p] = load_typed<1>(a.type, a.rows, (int64_t)row * a.row_stride + (c < col_end ? c : 0))[0];
+            }
+        }
 #pragma unroll
         for (int p = 0; p < kColumns; ++p) {
             const int32_t c = c0 + p * lanes + lane;
@@ -100,7 +110,6 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
             if (c < col_end && sharer == 0) squares += sum[p] * sum[p];
         }
         if constexpr (STEP) {
-            const float lr = *a.lr;
             float rate = lr;
             if (a.state) {
                 part[threadIdx.x] = squares;
@@ -109,8 +118,8 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
                     if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
                     __syncthreads();
                 }
-                const float state = a.state[row] + part[0] / (float)a.dim;
-                __syncthreads();                  // (all have read it)
+                state += part[0] / (float)a.dim;
+                __syncthreads();                  // (all have read both)
                 if (threadIdx.x == 0) a.state[row] = state;
                 rate = lr / (sqrtf(state) + a.eps);
             }
@@ -119,7 +128,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
                 const int32_t c = c0 + p * lanes + lane;
                 if (c >= col_end || sharer != 0) continue;
                 const int64_t element = (int64_t)row * a.row_stride + c;
-                store_typed<1>(a.type, a.rows, element, load_typed<1>(a.type, a.rows, element) - sum[p] * rate);
+                store_typed<1>(a.type, a.rows, element, Floats<1>(weight[p] - sum[p] * rate));
             }
         } else if (sharer == 0 && index < a.cap) {
             if (c0 == 0 && lane == 0) a.out_slots[index] = row;
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 {
     constexpr bool STEP = WB != 0;
     __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
-    __shared__ uint32_t sums[kReduceBlock / kWave], part_heads[kReduceBlock], part_flags[kReduceBlock], tile_shares;
+    __shared__ uint32_t sums[kReduceBlock / kWave], part_heads[kReduceBlock], part_flags[kReduceBlock], joins;
     __shared__ Floats<V> shares[NP][kReduceBlock];
 
     const int32_t tile_index = (int32_t)(blockIdx.x / (uint32_t)a.col_blocks), block_col = (int32_t)(blockIdx.x % (uint32_t)a.col_blocks);
@@ -158,7 +167,6 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     if (threadIdx.x == 0) {
         row_of_entry[0] = first > 0 ? row_at(a.entries, first - 1) : kNoRow;
         row_of_entry[m + behind + 1] = first + m + behind < a.n ? row_at(a.entries, first + m + behind) : kNoRow;
-        tile_shares = 0;
     }
     // runs before the tile
     uint32_t index = 0;
@@ -248,6 +256,16 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         for (int p = 0; p < NP; ++p)
             if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor);
     };
+    auto emit_row = [&](uint32_t row, uint32_t at) {
+        if constexpr (STEP) {
+            Weights w[NP];
+            float state;
+            load_weights(row, w, state);
+            emit_step(row, w, state);
+        } else {
+            emit_grad(row, at);
+        }
+    };
     // (unconditional loads, so that all that are asked for are under way at a time: where nothing is wanted, of a row that is in the
     // caches anyway; a lane without columns has the first one)
     typedef Raw<sizeof(TG), V> Gradient;
@@ -315,93 +333,149 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     if (lane == 0) part_flags[group] = flags;
     __syncthreads();
 
-    // The run that the part leaves unfinished, and (first group) the one that came from the tile before.
-    for (int which = 0; which < 2; ++which) {
-        const bool tail = which == 0;
-        if (tail ? !(flags & kTailShare) : group != 0 || !(part_flags[0] & kHeadShare)) continue;
-        const uint32_t row = row_of_entry[tail ? end : 1];
-        int g = group + 1;
-        if (!tail) {
-            g = 0;
+    // The shares of the parts from g on, as far as `on` says when it is asked for each, in their order; several are read at a time.
+    constexpr int kShares = NP * V >= 16 ? 2 : NP * V >= 8 ? 4 : 8;
+    auto add_shares = [&](Floats<V> (&to)[NP], int g, int count, auto on) {
+        bool goes_on = true;
+        while (g < count && goes_on) {
+            Floats<V> v[kShares][NP];
+            bool next[kShares];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) sum[p] = Floats<V>(0.f);
-        }
-        bool goes_on = true;                     // shares of the parts from g on, as far as the run goes
-        for (; g < groups && goes_on; ++g) {
+            for (int u = 0; u < kShares; ++u) {
+                const int at = g + u < count ? g + u : count - 1;
+                next[u] = on(at);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) sum[p] += shares[p][g * a.lanes + lane];
-            goes_on = part_flags[g] & kThrough;
-        }
-        if (goes_on && !long_run) {              // the entries behind the tile
-            for (int k0 = m; row_of_entry[k0 + 1] == row; k0 += kAhead) {
-                Gradient v[kAhead][NP];
-                uint32_t at[kAhead];
+                for (int p = 0; p < NP; ++p) v[u][p] = shares[p][at * a.lanes + lane];
+            }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    at[u] = position[k0 + u < m + behind ? k0 + u : m];
-                    load_grad(at[u], v[u]);
+            for (int u = 0; u < kShares; ++u) {
+                if (g + u < count && goes_on) {
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) to[p] += v[u][p];
+                    goes_on = next[u];
                 }
+            }
+            g += kShares;
+        }
+        return goes_on;
+    };
+    const auto through = [&](int g) -> bool { return part_flags[g] & kThrough; };
+
+    // The run that the part leaves unfinished, and (first group) the one that came from the tile before: their sums so far.
+    const bool finishes = leaves && !long_run;   // (the same for the whole workgroup)
+    bool unfinished = false, head_goes_on = false;
+    Floats<V> head_sum[NP];
+    if (flags & kTailShare) {
+        unfinished = add_shares(sum, group + 1, groups, through);
+        if (!unfinished) emit_row(row_of_entry[end], index - 1);
+    }
+    const bool has_head = group == 0 && (part_flags[0] & kHeadShare);
+    if (has_head) {
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u)
-                    if (k0 + u < m + behind && row_of_entry[k0 + u + 1] == row) add(v[u], at[u]);
-                if (k0 + kAhead >= m + behind) break;
-            }
-        }
-        if (tail && !(goes_on && long_run)) {
-            if constexpr (STEP) {
-                Weights w[NP];
-                float state;
-                load_weights(row, w, state);
-                emit_step(row, w, state);
-            } else {
-                emit_grad(row, index - 1);
-            }
-            continue;
-        }
-        float *to = (tail ? a.tail : a.head) + (int64_t)tile_index * a.dim;
+        for (int p = 0; p < NP; ++p) head_sum[p] = Floats<V>(0.f);
+        head_goes_on = add_shares(head_sum, 0, groups, through);
+    }
+    if (finishes) {                              // the entries behind the tile, a part of them for every group
+        __syncthreads();
+        const int share = (kBehind + groups - 1) / groups;
+        const int from = m + group * share, to = from + share < m + behind ? from + share : m + behind;
+        Floats<V> kept[NP];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            if (column[p] >= a.dim) continue;
+            kept[p] = sum[p];
+            sum[p] = Floats<V>(0.f);
+        }
+        for (int k0 = from; k0 < to && row_of_entry[k0 + 1] == tile_end_row; k0 += kAhead) {
+            Gradient v[kAhead][NP];
+            uint32_t at[kAhead];
 #pragma unroll
-            for (int e = 0; e < V; ++e) store_shared(to + column[p] + e, sum[p][e]);
+            for (int u = 0; u < kAhead; ++u) {
+                at[u] = position[k0 + u < to ? k0 + u : from];
+                load_grad(at[u], v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (k0 + u < to && row_of_entry[k0 + u + 1] == tile_end_row) add(v[u], at[u]);
         }
-        if (lane == 0) {
-            if (tail && block_col == 0) store_shared(a.tail_index + tile_index, index - 1);
-            atomicOr(&tile_shares, tail ? kTailShare : kHeadShare);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            shares[p][threadIdx.x] = sum[p];
+            sum[p] = kept[p];
         }
+        __syncthreads();
+        // (a part's share counts if the run reaches its first entry; the first one's does)
+        const int parts = (behind + share - 1) / share;
+        const auto reaches_next = [&](int g) { return g + 1 < parts && row_of_entry[m + (g + 1) * share + 1] == tile_end_row; };
+        if (unfinished) add_shares(sum, 0, parts, reaches_next);
+        if (head_goes_on) add_shares(head_sum, 0, parts, reaches_next);
+        if (unfinished) emit_row(tile_end_row, index - 1);
+        unfinished = false;
     }
-    wait_for_stores();
-    __syncthreads();
-    const uint32_t written = tile_shares;
-    if (!written) return;
-
-    // The shares are in memory before the counter says so, and the last workgroup of a run reads them behind it.
-    float *const part = reinterpret_cast<float *>(&shares[0][0]);
+    // Shares go to memory by way of LDS, so that neighbouring lanes store neighbouring elements (past the L2s every store is a
+    // transaction of its own).  They are there before the counter says so, and the last workgroup of a run reads them behind it.
+    const bool head_share = begins_inside && !finished && row_of_entry[1] != a.num_rows;
+    const bool tail_share = long_run && !(begins_inside && tile_end_row == row_of_entry[1]);
+    if (!head_share && !tail_share) return;
     const int32_t col_first = block_col * NP * V * a.lanes;
-    const int32_t col_end = col_first + NP * V * a.lanes < a.dim ? col_first + NP * V * a.lanes : a.dim;
-    for (uint32_t share = kHeadShare; share <= kTailShare; share <<= 2) {
-        if (!(written & share)) continue;        // (the same for the whole workgroup)
-        const uint32_t row = share == kHeadShare ? row_of_entry[1] : tile_end_row;
-        // the tile in which the run begins, and the last one that it goes into by more than kBehind entries
-        int32_t owner = tile_index;
-        if (share == kHeadShare) {
-            owner = wave_search<false>(a.tiles, row, [&](int32_t t) { return row_at(a.entries, (int64_t)t * a.tile); });
-            if (owner > 0 && row_at(a.entries, (int64_t)owner * a.tile - 1) == row) --owner;       // (it begins at a tile's begin, or inside one)
-        }
-        const int32_t last = wave_search<true>(a.tiles, row, [&](int32_t t) {
+    const int32_t columns = NP * V * a.lanes < a.dim - col_first ? NP * V * a.lanes : a.dim - col_first;
+    float *const part = reinterpret_cast<float *>(&shares[0][0]);        // (room for eight groups' sums)
+    __syncthreads();
+    auto keep = [&](float *to, const Floats<V> (&v)[NP]) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < V; ++e) to[(p * a.lanes + lane) * V + e] = v[p][e];
+    };
+    if (unfinished) {
+        keep(part, sum);
+        if (lane == 0 && block_col == 0) store_shared(a.tail_index + tile_index, index - 1);
+    }
+    if (has_head) keep(part + NP * V * a.lanes, head_sum);
+    __syncthreads();
+    for (int32_t c = threadIdx.x; c < columns; c += kReduceBlock) {
+        if (tail_share) store_shared(a.tail + (int64_t)tile_index * a.dim + col_first + c, part[c]);
+        if (head_share) store_shared(a.head + (int64_t)tile_index * a.dim + col_first + c, part[NP * V * a.lanes + c]);
+    }
+    // (meanwhile) the tile in which a run begins, and the last one that it goes into by more than kBehind entries: most of them are
+    // among the 63 tiles on either side, at which a wavefront looks at once
+    auto extent = [&](bool head, uint32_t row, int32_t &owner, int32_t &last) {
+        const auto begin_row = [&](int32_t t) { return row_at(a.entries, (int64_t)t * a.tile); };
+        const auto behind_row = [&](int32_t t) {
             const int64_t i = (int64_t)t * a.tile + kBehind;
             return i < a.n ? row_at(a.entries, i) : kNoRow;
-        }) - 1;
+        };
+        const int32_t before = tile_index - lane_id(), after = tile_index + lane_id();
+        const bool inside = head && before > 0 && begin_row(before) == row && row_at(a.entries, (int64_t)before * a.tile - 1) == row;
+        const bool goes_into = after < a.tiles && behind_row(after) <= row;
+        const uint64_t runs_into = __ballot(inside), reaches = __ballot(goes_into);
+        owner = tile_index - (int32_t)__popcll(runs_into);
+        if (~runs_into == 0) {
+            owner = wave_search<false>(a.tiles, row, begin_row);
+            if (owner > 0 && row_at(a.entries, (int64_t)owner * a.tile - 1) == row) --owner;       // (it begins at a tile's begin, or inside one)
+        }
+        last = tile_index + (int32_t)__popcll(reaches) - 1;
+        if (~reaches == 0) last = wave_search<true>(a.tiles, row, behind_row) - 1;
+    };
+    int32_t head_owner = 0, head_last = 0, tail_owner = 0, tail_last = 0;
+    if (head_share) extent(true, row_of_entry[1], head_owner, head_last);
+    if (tail_share) extent(false, tile_end_row, tail_owner, tail_last);
+    wait_for_stores();
+    __syncthreads();
+    for (int which = 0; which < 2; ++which) {
+        const bool head = which == 0;
+        if (!(head ? head_share : tail_share)) continue;
+        const uint32_t row = head ? row_of_entry[1] : tile_end_row;
+        const int32_t owner = head ? head_owner : tail_owner, last = head ? head_last : tail_last;
         __syncthreads();
         if (threadIdx.x == 0) {
             uint32_t *counter = a.arrived + (int64_t)owner * a.col_blocks + block_col;
             const bool is_last = atomicAdd(counter, 1u) == (uint32_t)(last - owner);
             if (is_last) store_shared(counter, 0u);
-            tile_shares = is_last;
+            joins = is_last;
         }
         __syncthreads();
-        if (!tile_shares) continue;
-        join_run<STEP>(a, part, row, owner, last, col_first, col_end);
+        if (!joins) continue;
+        join_run<STEP>(a, part, row, owner, last, col_first, col_first + columns);
         __syncthreads();
     }
 }
