@@ -56,7 +56,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
                                          int32_t col_end)
 {
     constexpr int kColumns = 2;                  // of a lane at a time; a step has the whole row at once
-    constexpr int kJoinAhead = 8;
+    constexpr int kJoinAhead = 16;
     static_assert(!STEP || kColumns * kReduceBlock >= MPZCH_MAX_STEP_DIM);
     int32_t lanes = kWave;
     while (lanes < kReduceBlock && lanes < col_end - col_first) lanes *= 2;
@@ -146,8 +146,9 @@ template <typename TG, int V, int NP, int WB>
 __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 {
     constexpr bool STEP = WB != 0;
+    constexpr int kWaves = kReduceBlock / kWave;
     __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
-    __shared__ uint32_t sums[kReduceBlock / kWave], part_heads[kReduceBlock], part_flags[kReduceBlock], joins;
+    __shared__ uint32_t heads_before[kWaves], heads_here[kWaves], wave_through[kWaves], joins;
     __shared__ Floats<V> shares[NP][kReduceBlock];
 
     const int32_t tile_index = (int32_t)(blockIdx.x / (uint32_t)a.col_blocks), block_col = (int32_t)(blockIdx.x % (uint32_t)a.col_blocks);
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     const int m = (int)(left < a.tile ? left : a.tile);
     const int behind = (int)(left - m < kBehind ? left - m : kBehind);
     const int groups = kReduceBlock / a.lanes, per = a.tile / groups;
-    const int group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
+    const int group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes, wave = threadIdx.x / kWave;
 
     // the tile's entries and the next ones, the row before them and the one behind
     for (int k = threadIdx.x; k < m + behind; k += kReduceBlock) {
@@ -168,40 +169,47 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         row_of_entry[0] = first > 0 ? row_at(a.entries, first - 1) : kNoRow;
         row_of_entry[m + behind + 1] = first + m + behind < a.n ? row_at(a.entries, first + m + behind) : kNoRow;
     }
-    // runs before the tile
-    uint32_t index = 0;
-    if constexpr (!STEP) {
-        if (a.heads_are == kBeforeTile) {
-            index = a.heads[tile_index];
-        } else {
-            uint32_t mine = 0;
-            if (a.heads_are == kOfTile)
-                for (int t = threadIdx.x; t < tile_index; t += kReduceBlock) mine += a.heads[t];
-            else
-#pragma unroll 4
-                for (int64_t i = threadIdx.x; i < first; i += kReduceBlock) {
-                    const uint32_t row = row_at(a.entries, i);
-                    mine += row != a.num_rows && (i == 0 || row_at(a.entries, i - 1) != row);
-                }
-            block_prefix(mine, sums, &index);
-        }
-    }
-    part_heads[threadIdx.x] = 0;
     __syncthreads();
     const int begin = group * per < m ? group * per : m, end = begin + per < m ? begin + per : m;
+    // `index`: runs that begin before the part
+    uint32_t index = 0;
     if constexpr (!STEP) {
-        uint32_t mine = 0;
+        uint32_t earlier = 0, mine = 0;          // in the tiles before this, one lane's share; in this part
+        if (a.heads_are == kOfTile) {
+            for (int t = threadIdx.x; t < tile_index; t += kReduceBlock) earlier += a.heads[t];
+        } else if (a.heads_are == kCountHere) {
+#pragma unroll 4
+            for (int64_t i = threadIdx.x; i < first; i += kReduceBlock) {
+                const uint32_t row = row_at(a.entries, i);
+                earlier += row != a.num_rows && (i == 0 || row_at(a.entries, i - 1) != row);
+            }
+        } else if (threadIdx.x == 0) {
+            earlier = a.heads[tile_index];
+        }
         for (int k = begin + lane; k < end; k += a.lanes)
             mine += row_of_entry[k + 1] != a.num_rows && row_of_entry[k + 1] != row_of_entry[k];
         for (int d = 1; d < a.lanes; d <<= 1) mine += __shfl_xor(mine, d);
-        if (lane == 0) part_heads[group] = mine;
+        uint32_t upto = mine;                    // of the wavefront's parts
+        for (int d = a.lanes; d < kWave; d <<= 1) {
+            const uint32_t x = __shfl_up(upto, d);
+            if (lane_id() >= d) upto += x;
+        }
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) earlier += __shfl_xor(earlier, d);
+        if (lane_id() == kWave - 1) {
+            heads_before[wave] = earlier;
+            heads_here[wave] = upto;
+        }
         __syncthreads();
-        uint32_t all;
-        const uint32_t before = block_prefix(part_heads[threadIdx.x], sums, &all);
-        part_heads[threadIdx.x] = before;
-        __syncthreads();
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            index += heads_before[w];
+            if (w < wave) index += heads_here[w];
+            all += heads_here[w];
+        }
         if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *a.out_count = (int64_t)index + all;
-        index += part_heads[group];
+        index += upto - mine;
     }
     // what is left out: padding, and the rest of a run that an earlier tile has finished
     const uint32_t tile_end_row = m > 0 ? row_of_entry[m] : kNoRow;
@@ -330,53 +338,65 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             }
         }
     }
-    if (lane == 0) part_flags[group] = flags;
+
+    // A chain is the shares of following parts as far as a run goes: first inside every wavefront, from each of its parts to its
+    // end, by doubling; the chains from the wavefronts' first parts then go to LDS.
+    const int in_wave = kWave / a.lanes, place = group % in_wave;
+    Floats<V> chain[NP];
+    bool through = flags & kThrough;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) chain[p] = flags & kHeadShare ? shares[p][threadIdx.x] : Floats<V>(0.f);
+    for (int d = 1; d < in_wave; d <<= 1) {
+        const bool next = __shfl_down((int)through, d * a.lanes);
+        const bool adds = through && place + d < in_wave;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float x = __shfl_down(chain[p][e], d * a.lanes);
+                if (adds) chain[p][e] += x;
+            }
+        if (adds) through = next;
+    }
+    if (place == 0) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) shares[p][threadIdx.x] = chain[p];
+        if (lane == 0) wave_through[wave] = through;
+    }
+    // the run that the part leaves unfinished goes on with the next part's chain
+    const bool had_tail = flags & kTailShare;
+    bool unfinished = had_tail;
+    {
+        const bool next = __shfl_down((int)through, a.lanes);
+        const bool adds = had_tail && place + 1 < in_wave;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float x = __shfl_down(chain[p][e], a.lanes);
+                if (adds) sum[p][e] += x;
+            }
+        if (adds) unfinished = next;
+    }
     __syncthreads();
-
-    // The shares of the parts from g on, as far as `on` says when it is asked for each, in their order; several are read at a time.
-    constexpr int kShares = NP * V >= 16 ? 2 : NP * V >= 8 ? 4 : 8;
-    auto add_shares = [&](Floats<V> (&to)[NP], int g, int count, auto on) {
-        bool goes_on = true;
-        while (g < count && goes_on) {
-            Floats<V> v[kShares][NP];
-            bool next[kShares];
+    auto follow = [&](Floats<V> (&to)[NP], int w) {      // ... and with those of the wavefronts from w on; whether it leaves the tile
+        int until = w;
+        while (until < kWaves && wave_through[until]) ++until;
+        const int last = until < kWaves ? until : kWaves - 1;
+#pragma unroll 2
+        for (int i = w; i <= last; ++i)
 #pragma unroll
-            for (int u = 0; u < kShares; ++u) {
-                const int at = g + u < count ? g + u : count - 1;
-                next[u] = on(at);
-#pragma unroll
-                for (int p = 0; p < NP; ++p) v[u][p] = shares[p][at * a.lanes + lane];
-            }
-#pragma unroll
-            for (int u = 0; u < kShares; ++u) {
-                if (g + u < count && goes_on) {
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) to[p] += v[u][p];
-                    goes_on = next[u];
-                }
-            }
-            g += kShares;
-        }
-        return goes_on;
+            for (int p = 0; p < NP; ++p) to[p] += shares[p][i * kWave + lane];
+        return until == kWaves;
     };
-    const auto through = [&](int g) -> bool { return part_flags[g] & kThrough; };
+    if (unfinished) unfinished = follow(sum, wave + 1);
+    if (had_tail && !unfinished) emit_row(row_of_entry[end], index - 1);
+    // the run that came from the tile before
+    const bool has_head = group == 0 && (flags & kHeadShare);
+    const bool head_goes_on = has_head && through && follow(chain, 1);
 
-    // The run that the part leaves unfinished, and (first group) the one that came from the tile before: their sums so far.
     const bool finishes = leaves && !long_run;   // (the same for the whole workgroup)
-    bool unfinished = false, head_goes_on = false;
-    Floats<V> head_sum[NP];
-    if (flags & kTailShare) {
-        unfinished = add_shares(sum, group + 1, groups, through);
-        if (!unfinished) emit_row(row_of_entry[end], index - 1);
-    }
-    const bool has_head = group == 0 && (part_flags[0] & kHeadShare);
-    if (has_head) {
-#pragma unroll
-        for (int p = 0; p < NP; ++p) head_sum[p] = Floats<V>(0.f);
-        head_goes_on = add_shares(head_sum, 0, groups, through);
-    }
     if (finishes) {                              // the entries behind the tile, a part of them for every group
-        __syncthreads();
         const int share = (kBehind + groups - 1) / groups;
         const int from = m + group * share, to = from + share < m + behind ? from + share : m + behind;
         Floats<V> kept[NP];
@@ -397,17 +417,29 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             for (int u = 0; u < kAhead; ++u)
                 if (k0 + u < to && row_of_entry[k0 + u + 1] == tile_end_row) add(v[u], at[u]);
         }
+        for (int d = a.lanes; d < kWave; d <<= 1)
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            shares[p][threadIdx.x] = sum[p];
-            sum[p] = kept[p];
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[p][e] += __shfl_xor(sum[p][e], d);
+        __syncthreads();                         // (the chains have been read)
+        if (place == 0) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) shares[p][threadIdx.x] = sum[p];
         }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) sum[p] = kept[p];
         __syncthreads();
-        // (a part's share counts if the run reaches its first entry; the first one's does)
-        const int parts = (behind + share - 1) / share;
-        const auto reaches_next = [&](int g) { return g + 1 < parts && row_of_entry[m + (g + 1) * share + 1] == tile_end_row; };
-        if (unfinished) add_shares(sum, 0, parts, reaches_next);
-        if (head_goes_on) add_shares(head_sum, 0, parts, reaches_next);
+        if (unfinished || head_goes_on) {
+#pragma unroll 2
+            for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const Floats<V> x = shares[p][w * kWave + lane];
+                    if (unfinished) sum[p] += x;
+                    else chain[p] += x;
+                }
+        }
         if (unfinished) emit_row(tile_end_row, index - 1);
         unfinished = false;
     }
@@ -430,7 +462,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         keep(part, sum);
         if (lane == 0 && block_col == 0) store_shared(a.tail_index + tile_index, index - 1);
     }
-    if (has_head) keep(part + NP * V * a.lanes, head_sum);
+    if (has_head) keep(part + NP * V * a.lanes, chain);
     __syncthreads();
     for (int32_t c = threadIdx.x; c < columns; c += kReduceBlock) {
         if (tail_share) store_shared(a.tail + (int64_t)tile_index * a.dim + col_first + c, part[c]);
