@@ -96,7 +96,6 @@ mpzch_status_t launch_embed(const EmbedArgs &a, int32_t out_type, int width, int
 constexpr int64_t kReduceWaves = 8192;
 constexpr int kPartMin = 4;
 constexpr int64_t kTilesAdded = 2048;        // up to which a workgroup itself adds up the heads of the tiles before its own
-constexpr int64_t kWideDigits = 1 << 17;
 
 struct ReducePlan {
     int lanes, pieces, col_blocks, tile, tiles;      // pieces: of a lane, as compiled
@@ -129,29 +128,32 @@ int64_t most_tiles(int64_t n)
 }
 int64_t most_col_blocks(int64_t dim) { return ceil_div(dim, kWave * 16); }
 
-// How a batch is sorted: by its ranks, or in passes over tiles.
-constexpr int kFewTiles = 64;
+// How a batch is sorted beyond kRankMax.  Few tiles leave compute units idle, many take the workgroups long to add up; passes are
+// launches.  us, whole calls, by entries of a lane (1, 2, 4): a step of 65 536 39.3 39.4 43.1, gradients of 20 011 31.1 33.1 37.3 and
+// of 300 007 79 67 72, steps of 1 M - 190 184, gradients of 2 M - 330 307 (and 8: 309).
+constexpr int64_t kWideMost = 65536;         // digits of kWideBits: two passes for a million rows (39.3 us instead of 41.3)
+constexpr int64_t kTwoMost = 524288;         // two entries a lane up to here, four beyond
+constexpr int kFewTiles = 256;               // added up by every workgroup; beyond, by a launch (147 tiles 67 and 76 us, 489 346 and 306)
 struct SortPlan {
-    int passes, bits, items, tiles;
+    int passes, bits, tiles;
 };
 SortPlan sort_plan(int64_t n, int64_t num_rows)
 {
     int bits = 0;
     while (num_rows >> bits) ++bits;             // (padding has the row num_rows)
-    const int widest = n <= kWideDigits ? kMaxDigitBits : 9;
     SortPlan p;
-    p.passes = (int)ceil_div(bits, widest);
+    p.passes = (int)ceil_div(bits, n <= kWideMost ? kWideBits : kNarrowBits);
     p.bits = (int)ceil_div(bits, p.passes);
-    if (p.bits < 6) p.bits = 6;
-    p.items = n <= kWideDigits ? 4 : 8;
-    p.tiles = (int)ceil_div(n, kSortBlock * p.items);
+    if ((1 << p.bits) < kScanDigits) p.bits = 6;
+    p.tiles = (int)ceil_div(n, kSortBlock * (n <= kWideMost ? 1 : n <= kTwoMost ? 2 : 4));
     return p;
 }
 // words of the histograms (and twice that, and a tile more, of their scan) that any batch of up to n positions needs
 int64_t hist_words(int64_t n)
 {
-    const int64_t wide = ceil_div(n < kWideDigits ? n : kWideDigits, kSortBlock * 4) * (kMaxDigits / 2);
-    const int64_t narrow = ceil_div(n, kSortBlock * 8) * (512 / 2);
+    const int64_t wide = kWideMost / kSortBlock << (kWideBits - 1);
+    const int64_t two = ceil_div(n < kTwoMost ? n : kTwoMost, 2 * kSortBlock), four = ceil_div(n, 4 * kSortBlock);
+    const int64_t narrow = (two > four ? two : four) << (kNarrowBits - 1);
     return wide > narrow ? wide : narrow;
 }
 
@@ -173,7 +175,7 @@ size_t lay_out(int64_t n, int64_t dim, char *base, Areas *out)
     out->entries[0] = (uint64_t *)take(8 * (size_t)n);
     out->entries[1] = (uint64_t *)take(8 * (size_t)n);
     out->hist = (uint32_t *)take(4 * (size_t)hist_words(n));
-    out->before = (uint32_t *)take(8 * ((size_t)hist_words(n) + kMaxDigits / 2));
+    out->before = (uint32_t *)take(8 * ((size_t)hist_words(n) + (1 << (kNarrowBits - 1))));
     out->heads = (uint32_t *)take(4 * (size_t)tiles);
     out->tail_index = (uint32_t *)take(4 * (size_t)tiles);
     out->arrived = (uint32_t *)take(arrived_bytes(n, dim));
@@ -217,17 +219,23 @@ mpzch_status_t ensure(mpzch_embed_t *h, int64_t n, int64_t dim)
     return MPZCH_OK;
 }
 
+template <bool FIRST, int ITEMS, int BITS>
+mpzch_status_t sort_pass(const Areas &w, const SortPlan &p, const SortSource &src, uint64_t *to, hipStream_t s)
+{
+    TRY(launch(k_sort_hist<FIRST, ITEMS, BITS>, p.tiles, kSortBlock, s, src, w.hist));
+    const uint32_t *before = nullptr;
+    if (p.tiles > kFewTiles) {
+        before = w.before;
+        TRY(launch(k_sort_scan, (1 << p.bits) / kScanDigits, kSortBlock, s, (const uint32_t *)w.hist, w.before, p.tiles, p.bits));
+    }
+    return launch(k_sort_scatter<FIRST, ITEMS, BITS>, p.tiles, kSortBlock, s, src, (const uint32_t *)w.hist, before, p.tiles, to);
+}
 template <bool FIRST>
 mpzch_status_t sort_pass(const Areas &w, const SortPlan &p, const SortSource &src, uint64_t *to, hipStream_t s)
 {
-    const bool few = p.tiles <= kFewTiles;
-    if (p.items == 4) TRY(launch(k_sort_hist<FIRST, 4>, p.tiles, kSortBlock, s, src, w.hist));
-    else TRY(launch(k_sort_hist<FIRST, 8>, p.tiles, kSortBlock, s, src, w.hist));
-    if (!few) TRY(launch(k_sort_scan, 1 << (p.bits - 6), kSortBlock, s, (const uint32_t *)w.hist, w.before, p.tiles, src.bits));
-    const uint32_t *before = few ? nullptr : w.before;
-    if (p.items == 4) TRY(launch(k_sort_scatter<FIRST, 4>, p.tiles, kSortBlock, s, src, (const uint32_t *)w.hist, before, p.tiles, to));
-    else TRY(launch(k_sort_scatter<FIRST, 8>, p.tiles, kSortBlock, s, src, (const uint32_t *)w.hist, before, p.tiles, to));
-    return MPZCH_OK;
+    if (src.n <= kWideMost) return sort_pass<FIRST, 1, kWideBits>(w, p, src, to, s);
+    if (src.n <= kTwoMost) return sort_pass<FIRST, 2, kNarrowBits>(w, p, src, to, s);
+    return sort_pass<FIRST, 4, kNarrowBits>(w, p, src, to, s);
 }
 
 // entries in ascending order; *out: where they are

@@ -63,13 +63,16 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
 // Longer ones: a radix sort, least significant digit first, each pass stable, so that the positions of a row stay ascending.
 // A pass counts the digits of every tile (k_sort_hist), adds up what earlier tiles hold (k_sort_scan; where there are few
 // tiles, k_sort_scatter itself) and moves the entries (k_sort_scatter).
-constexpr int kMaxDigitBits = 11, kMaxDigits = 1 << kMaxDigitBits;
+// Digits of up to kWideBits bits where passes are few launches after all, of kNarrowBits where there are many entries to move: the
+// more digits, the shorter the stretches that a tile stores side by side.
+constexpr int kWideBits = 11, kNarrowBits = 9;
+constexpr int kScanDigits = 64;
 
 // hist[tile][digit]: how many entries of the tile have the digit, 16 bits each
-template <bool FIRST, int ITEMS>
+template <bool FIRST, int ITEMS, int BITS>
 __global__ __launch_bounds__(kSortBlock) void k_sort_hist(SortSource s, uint32_t *hist)
 {
-    __shared__ uint32_t count[kMaxDigits];
+    __shared__ uint32_t count[1 << BITS];
     const uint32_t digits = 1u << s.bits;
     for (uint32_t d = threadIdx.x; d < digits; d += kSortBlock) count[d] = 0;
     __syncthreads();
@@ -80,9 +83,18 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_hist(SortSource s, uint32_t
         const int64_t i = first + u * kSortBlock + threadIdx.x;
         entry[u] = i < s.n ? sort_entry<FIRST>(s, i) : 0;
     }
+    // (entries of a frequent row lie side by side behind the first pass: a wavefront with one digit adds it once)
 #pragma unroll
-    for (int u = 0; u < ITEMS; ++u)
-        if (first + u * kSortBlock + threadIdx.x < s.n) atomicAdd(&count[(uint32_t)(entry[u] >> s.shift) & (digits - 1)], 1u);
+    for (int u = 0; u < ITEMS; ++u) {
+        const uint32_t digit = (uint32_t)(entry[u] >> s.shift) & (digits - 1);
+        const bool there = first + u * kSortBlock + threadIdx.x < s.n;
+        const uint64_t same = __ballot(there && digit == (uint32_t)__builtin_amdgcn_readfirstlane((int)digit));
+        if (same == __ballot(there)) {
+            if (there && lane_id() == 0) atomicAdd(&count[digit], (uint32_t)__popcll(same));
+        } else if (there) {
+            atomicAdd(&count[digit], 1u);
+        }
+    }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < digits / 2; d += kSortBlock)
         hist[(int64_t)blockIdx.x * (digits / 2) + d] = count[2 * d] | count[2 * d + 1] << 16;
@@ -90,7 +102,6 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_hist(SortSource s, uint32_t
 
 // before[tile][digit]: entries of earlier tiles with the digit; behind the last tile the entries of all.  A workgroup has 64 digits,
 // each lane two of them and a 32nd of the tiles.
-constexpr int kScanDigits = 64;
 __global__ __launch_bounds__(kSortBlock) void k_sort_scan(const uint32_t *hist, uint32_t *before, int32_t tiles, int32_t bits)
 {
     __shared__ uint32_t low[32][32], high[32][32];
@@ -127,21 +138,23 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scan(const uint32_t *hist, 
 // Every wavefront ranks its entries 64 at a time: the lanes with the same digit find each other by ballots over the digit's
 // bits, the first of them adds their number to the wavefront's count in LDS (its own, so the order of its accesses is that of
 // the program).  The entries then go to LDS in their new order, so that neighbouring lanes store neighbouring entries.
-template <bool FIRST, int ITEMS>
+template <bool FIRST, int ITEMS, int BITS>
 __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const uint32_t *hist, const uint32_t *before, int32_t tiles,
                                                               uint64_t *out)
 {
     constexpr int kTile = kSortBlock * ITEMS;
     // the counts of the wavefronts, 16 bits each, and then the entries
-    constexpr int kCountBytes = kSortWaves * kMaxDigits * 2, kEntryBytes = kTile * 8;
+    constexpr int kCountBytes = kSortWaves * (2 << BITS), kEntryBytes = kTile * 8;
     __shared__ __align__(16) unsigned char area[kCountBytes > kEntryBytes ? kCountBytes : kEntryBytes];
-    __shared__ uint16_t local[kMaxDigits];         // (two workgroups on a compute unit)
-    __shared__ uint32_t global[kMaxDigits], sums[kSortWaves];
+    __shared__ uint32_t earlier[1 << BITS], all[1 << BITS], sums[2][kSortWaves];
+    uint32_t *const global = earlier, *const local = all;
     uint16_t *const count = reinterpret_cast<uint16_t *>(area);
     uint64_t *const sorted = reinterpret_cast<uint64_t *>(area);
     const uint32_t digits = 1u << s.bits, pairs = digits / 2;
     const int wave = threadIdx.x / kWave, lane = lane_id();
     for (uint32_t k = threadIdx.x; k < kSortWaves * pairs / 4; k += kSortBlock) reinterpret_cast<u32x4 *>(area)[k] = u32x4(0);
+    if (!before)
+        for (uint32_t d = threadIdx.x; d < digits; d += kSortBlock) earlier[d] = all[d] = 0;
     const int64_t first = (int64_t)blockIdx.x * kTile;
     const int64_t left = s.n - first;
     const int mine = (int)(left < kTile ? left : kTile);
@@ -152,25 +165,32 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const
         const int at = wave * (kWave * ITEMS) + u * kWave + lane;
         entry[u] = at < mine ? sort_entry<FIRST>(s, first + at) : 0;
     }
-    // what earlier tiles hold of this lane's two digits, and all tiles
-    uint32_t earlier[2] = {0, 0}, all[2] = {0, 0};
-    if (threadIdx.x < pairs) {
-        if (before) {
+    // what earlier tiles hold of two digits, and all tiles; where the tiles are added up here, by all lanes, a part of the tiles each
+    if (before) {
+        if (threadIdx.x < pairs) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                earlier[k] = before[((int64_t)blockIdx.x * pairs + threadIdx.x) * 2 + k];
-                all[k] = before[((int64_t)tiles * pairs + threadIdx.x) * 2 + k];
+                earlier[2 * threadIdx.x + k] = before[((int64_t)blockIdx.x * pairs + threadIdx.x) * 2 + k];
+                all[2 * threadIdx.x + k] = before[((int64_t)tiles * pairs + threadIdx.x) * 2 + k];
             }
-        } else {
+        }
+    } else {
+        const int parts = kSortBlock / pairs, pair = threadIdx.x % pairs;
+        uint32_t e[2] = {0, 0}, x[2] = {0, 0};
 #pragma unroll 8
-            for (int32_t t = 0; t < tiles; ++t) {
-                const uint32_t v = hist[(int64_t)t * pairs + threadIdx.x];
-                const uint32_t early = t < (int32_t)blockIdx.x ? v : 0;
-                earlier[0] += early & 0xFFFF;
-                earlier[1] += early >> 16;
-                all[0] += v & 0xFFFF;
-                all[1] += v >> 16;
-            }
+        for (int32_t t = threadIdx.x / pairs; t < tiles; t += parts) {
+            const uint32_t v = hist[(int64_t)t * pairs + pair];
+            const uint32_t early = t < (int32_t)blockIdx.x ? v : 0;
+            e[0] += early & 0xFFFF;
+            e[1] += early >> 16;
+            x[0] += v & 0xFFFF;
+            x[1] += v >> 16;
+        }
+        __syncthreads();                         // (the sums are empty)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            atomicAdd(&earlier[2 * pair + k], e[k]);
+            atomicAdd(&all[2 * pair + k], x[k]);
         }
     }
     __syncthreads();
@@ -204,14 +224,43 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const
                 sum += c[w];
             }
         }
-        uint32_t total;
-        const uint32_t here = block_prefix((sum & 0xFFFF) + (sum >> 16), sums, &total);
-        const uint32_t there = block_prefix(all[0] + all[1], sums, &total);
+        // exclusive prefixes over the digits, of this tile's counts and of all tiles'
+        uint32_t e[2] = {0, 0}, x[2] = {0, 0};
         if (threadIdx.x < pairs) {
-            local[2 * threadIdx.x] = (uint16_t)here;
-            local[2 * threadIdx.x + 1] = (uint16_t)(here + (sum & 0xFFFF));
-            global[2 * threadIdx.x] = there + earlier[0] - here;
-            global[2 * threadIdx.x + 1] = there + all[0] + earlier[1] - here - (sum & 0xFFFF);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                e[k] = earlier[2 * threadIdx.x + k];
+                x[k] = all[2 * threadIdx.x + k];
+            }
+        }
+        const uint32_t own = (sum & 0xFFFF) + (sum >> 16), every = x[0] + x[1];
+        uint32_t here = own, there = every;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t y = __shfl_up(here, d), z = __shfl_up(there, d);
+            if (lane >= d) {
+                here += y;
+                there += z;
+            }
+        }
+        if (lane == kWave - 1) {
+            sums[0][wave] = here;
+            sums[1][wave] = there;
+        }
+        __syncthreads();
+        here -= own;
+        there -= every;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w)
+            if (w < wave) {
+                here += sums[0][w];
+                there += sums[1][w];
+            }
+        if (threadIdx.x < pairs) {
+            local[2 * threadIdx.x] = here;
+            local[2 * threadIdx.x + 1] = here + (sum & 0xFFFF);
+            global[2 * threadIdx.x] = there + e[0] - here;
+            global[2 * threadIdx.x + 1] = there + x[0] + e[1] - here - (sum & 0xFFFF);
         }
     }
     __syncthreads();
