@@ -51,6 +51,9 @@ struct Rows {
     }
 };
 
+// results of this many bytes are stored past the caches: half of what the memory-side one holds
+constexpr int64_t kPastCaches = (int64_t)1 << 27;
+
 // scale and dropout of a call
 bool make_mask(float scale, double drop_p, const int64_t *seed, int64_t dim, float *factor, Mask *mask)
 {
@@ -93,7 +96,7 @@ mpzch_status_t launch_embed(const EmbedArgs &a, int32_t out_type, int width, int
 // ---- gradient -------------------------------------------------------------------------------
 // How the sums are shared out: kReduceWaves wavefronts or more, but no part of a tile shorter than kPartMin entries and no
 // tile longer than kReduceTile.
-constexpr int64_t kReduceWaves = 8192;
+constexpr int64_t kReduceWaves = 4096;
 constexpr int kPartMin = 4;
 constexpr int64_t kTilesAdded = 2048;        // up to which a workgroup itself adds up the heads of the tiles before its own
 
@@ -144,7 +147,7 @@ SortPlan sort_plan(int64_t n, int64_t num_rows)
     SortPlan p;
     p.passes = (int)ceil_div(bits, n <= kWideMost ? kWideBits : kNarrowBits);
     p.bits = (int)ceil_div(bits, p.passes);
-    if ((1 << p.bits) < kScanDigits) p.bits = 6;
+    if (p.bits < kLeastBits) p.bits = kLeastBits;
     p.tiles = (int)ceil_div(n, kSortBlock * (n <= kWideMost ? 1 : n <= kTwoMost ? 2 : 4));
     return p;
 }
@@ -322,6 +325,7 @@ mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n, const void *rows, in
     a.out = (char *)out;
     a.out_stride = out_stride_bytes;
     a.pieces = div32((uint32_t)(dim / width));
+    a.past_caches = n * dim * element_bytes(out_type) >= kPastCaches;
     hipStream_t s = (hipStream_t)stream;
     int num_cus = 0;
     TRY(device_cus(&num_cus));
@@ -379,6 +383,7 @@ mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t 
     a.out_count = out_count;
     a.out_rows = (char *)out_rows;
     a.cap = out_cap;
+    a.past_caches = (n < out_cap ? n : out_cap) * dim * element_bytes(out_type) >= kPastCaches;
     a.type = out_type;
     return run_gradient<false>(h, slots, n, num_rows, g, width, a, (hipStream_t)stream);
 }

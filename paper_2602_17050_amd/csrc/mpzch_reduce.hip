@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         if (block_col == 0 && lane == 0) a.out_slots[at] = row;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
-            if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor);
+            if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor, a.past_caches);
     };
     auto emit_row = [&](uint32_t row, uint32_t at) {
         if constexpr (STEP) {
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         }
     };
 
-    constexpr int kAhead = NP >= 8 ? 2 : 4;
+    constexpr int kAhead = NP > 1 ? 2 : 4;
     uint32_t flags = 0;
     bool from_before = begin < end && row_of_entry[begin] == row_of_entry[begin + 1];
     for (int k0 = begin; k0 < end; k0 += kAhead) {

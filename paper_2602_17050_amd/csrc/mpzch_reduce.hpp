@@ -29,6 +29,7 @@ struct ReduceArgs {
     int64_t *out_slots, *out_count;
     char *out_rows;
     int64_t cap;
+    bool past_caches;            // out_rows are stored non-temporally
     // step
     char *rows;
     int64_t row_stride;          // elements

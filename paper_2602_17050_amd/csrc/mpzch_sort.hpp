@@ -65,8 +65,8 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
 // tiles, k_sort_scatter itself) and moves the entries (k_sort_scatter).
 // Digits of up to kWideBits bits where passes are few launches after all, of kNarrowBits where there are many entries to move: the
 // more digits, the shorter the stretches that a tile stores side by side.
-constexpr int kWideBits = 11, kNarrowBits = 9;
-constexpr int kScanDigits = 64;
+constexpr int kWideBits = 11, kNarrowBits = 9, kLeastBits = 6;
+constexpr int kScanDigits = 16;
 
 // hist[tile][digit]: how many entries of the tile have the digit, 16 bits each
 template <bool FIRST, int ITEMS, int BITS>
@@ -100,14 +100,15 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_hist(SortSource s, uint32_t
         hist[(int64_t)blockIdx.x * (digits / 2) + d] = count[2 * d] | count[2 * d + 1] << 16;
 }
 
-// before[tile][digit]: entries of earlier tiles with the digit; behind the last tile the entries of all.  A workgroup has 64 digits,
-// each lane two of them and a 32nd of the tiles.
+// before[tile][digit]: entries of earlier tiles with the digit; behind the last tile the entries of all.  A workgroup has 16 digits,
+// each lane two of them and a 128th of the tiles; lanes with the same digits are 8 apart.
 __global__ __launch_bounds__(kSortBlock) void k_sort_scan(const uint32_t *hist, uint32_t *before, int32_t tiles, int32_t bits)
 {
-    __shared__ uint32_t low[32][32], high[32][32];
+    constexpr int kPairs = kScanDigits / 2, kParts = kSortBlock / kPairs;
+    __shared__ uint32_t sums[2][kSortWaves][kPairs];
     const int32_t pairs = 1 << (bits - 1);
-    const int32_t pair = (int32_t)blockIdx.x * (kScanDigits / 2) + (int32_t)(threadIdx.x & 31), part = threadIdx.x / 32;
-    const int32_t per = (tiles + 31) / 32, begin = part * per < tiles ? part * per : tiles, end = begin + per < tiles ? begin + per : tiles;
+    const int32_t mine = threadIdx.x % kPairs, pair = (int32_t)blockIdx.x * kPairs + mine, part = threadIdx.x / kPairs;
+    const int32_t per = (tiles + kParts - 1) / kParts, begin = part * per < tiles ? part * per : tiles, end = begin + per < tiles ? begin + per : tiles;
     uint32_t a = 0, b = 0;
 #pragma unroll 8
     for (int32_t t = begin; t < end; ++t) {
@@ -115,23 +116,41 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scan(const uint32_t *hist, 
         a += v & 0xFFFF;
         b += v >> 16;
     }
-    low[part][threadIdx.x & 31] = a;
-    high[part][threadIdx.x & 31] = b;
-    __syncthreads();
-    a = b = 0;
-    for (int32_t q = 0; q < part; ++q) {
-        a += low[q][threadIdx.x & 31];
-        b += high[q][threadIdx.x & 31];
+    uint32_t low = a, high = b;
+#pragma unroll
+    for (int d = kPairs; d < kWave; d <<= 1) {
+        const uint32_t x = __shfl_up(low, d), y = __shfl_up(high, d);
+        if (lane_id() >= d) {
+            low += x;
+            high += y;
+        }
     }
-    for (int32_t t = begin; t <= end; ++t) {
-        if (t == end && !(part == 31)) break;
+    const int wave = threadIdx.x / kWave;
+    if (lane_id() >= kWave - kPairs) {
+        sums[0][wave][mine] = low;
+        sums[1][wave][mine] = high;
+    }
+    __syncthreads();
+    low -= a;
+    high -= b;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w)
+        if (w < wave) {
+            low += sums[0][w][mine];
+            high += sums[1][w][mine];
+        }
+    for (int32_t t = begin; t < end; ++t) {
         uint32_t *to = before + ((int64_t)t * pairs + pair) * 2;
-        to[0] = a;
-        to[1] = b;
-        if (t == end) break;
+        to[0] = low;
+        to[1] = high;
         const uint32_t v = hist[(int64_t)t * pairs + pair];
-        a += v & 0xFFFF;
-        b += v >> 16;
+        low += v & 0xFFFF;
+        high += v >> 16;
+    }
+    if (part == kParts - 1) {                    // (its part ends with the last tile, if it is not empty behind it)
+        uint32_t *to = before + ((int64_t)tiles * pairs + pair) * 2;
+        to[0] = low;
+        to[1] = high;
     }
 }
 
@@ -177,14 +196,22 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const
     } else {
         const int parts = kSortBlock / pairs, pair = threadIdx.x % pairs;
         uint32_t e[2] = {0, 0}, x[2] = {0, 0};
-#pragma unroll 8
-        for (int32_t t = threadIdx.x / pairs; t < tiles; t += parts) {
-            const uint32_t v = hist[(int64_t)t * pairs + pair];
-            const uint32_t early = t < (int32_t)blockIdx.x ? v : 0;
-            e[0] += early & 0xFFFF;
-            e[1] += early >> 16;
-            x[0] += v & 0xFFFF;
-            x[1] += v >> 16;
+        for (int32_t t0 = threadIdx.x / pairs; t0 < tiles; t0 += 8 * parts) {
+            uint32_t v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int32_t t = t0 + u * parts;
+                v[u] = hist[(int64_t)(t < tiles ? t : t0) * pairs + pair];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int32_t t = t0 + u * parts;
+                const uint32_t counted = t < tiles ? v[u] : 0, early = t < (int32_t)blockIdx.x ? v[u] : 0;
+                e[0] += early & 0xFFFF;
+                e[1] += early >> 16;
+                x[0] += counted & 0xFFFF;
+                x[1] += counted >> 16;
+            }
         }
         __syncthreads();                         // (the sums are empty)
 #pragma unroll
