@@ -30,9 +30,9 @@ __device__ __forceinline__ Floats<V> load_floats(const char *at)
 {
     return __builtin_convertvector(*reinterpret_cast<const Pack<E, V> *>(at), Floats<V>);
 }
-// Rounded once, to nearest, ties to even.  past_caches: non-temporally, for results that the memory-side cache (256 MB) cannot keep
-// for the next kernel anyway and that would only drive out of it what this one reads again.  Lookup of 2 M rows of 256 bytes
-// 172 -> 129 us, gradient of as many (271 MB of sums) 307 -> 301; non-temporal loads of rows, which are read again: 219.
+// Rounded once, to nearest, ties to even.  past_caches: non-temporally, so that large results do not drive out of the caches what
+// is read again.  Lookup of 2 M rows of 256 bytes 172 -> 125 us, gradient of as many (271 MB of sums) 302 -> 297; non-temporal
+// loads of rows: 219.
 template <typename E, int V>
 __device__ __forceinline__ void store_floats(char *at, Floats<V> v, bool past_caches = false)
 {

@@ -30,6 +30,23 @@ __device__ __forceinline__ T load_shared(const T *at) { return __hip_atomic_load
 // this lane's stores have reached the memory that all dies see
 __device__ __forceinline__ void wait_for_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// the sum over the lanes of a group (a power of two of them, the same for the wavefront), in every lane
+template <int CONTROL>
+__device__ __forceinline__ float from_lane(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float group_sum(float x, int lanes)
+{
+    if (lanes > 1) x += from_lane<0xB1>(x);          // lanes 1 0 3 2
+    if (lanes > 2) x += from_lane<0x4E>(x);          // lanes 2 3 0 1
+    if (lanes > 4) x += from_lane<0x141>(x);         // the other four of eight, mirrored: they have one sum
+    if (lanes > 8) x += from_lane<0x140>(x);         // the other eight of sixteen
+    if (lanes > 16) x += __shfl_xor(x, 16);
+    if (lanes > 32) x += __shfl_xor(x, 32);
+    return x;
+}
+
 // how many of x(0) .. x(count - 1), ascending, are below v (or, with EQUAL, not above it): a wavefront looks at 64 of them at a time
 template <bool EQUAL, typename X>
 __device__ __forceinline__ int32_t wave_search(int32_t count, uint32_t v, X x)
@@ -51,11 +68,12 @@ __device__ __forceinline__ int32_t wave_search(int32_t count, uint32_t v, X x)
 
 // The sum of a run whose shares lie in the tiles owner .. last, by a whole workgroup: `lanes` lanes (a power of two) for the
 // columns of this block, and the rest of it for every sharers-th tile.
+constexpr int kJoinColumns = 2;              // of a lane at a time; a step has the whole row at once
 template <bool STEP>
 __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint32_t row, int32_t owner, int32_t last, int32_t col_first,
                                          int32_t col_end)
 {
-    constexpr int kColumns = 2;                  // of a lane at a time; a step has the whole row at once
+    constexpr int kColumns = kJoinColumns;
     constexpr int kJoinAhead = 16;
     static_assert(!STEP || kColumns * kReduceBlock >= MPZCH_MAX_STEP_DIM);
     int32_t lanes = kWave;
@@ -63,6 +81,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
     const int sharers = kReduceBlock / lanes, sharer = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     const int64_t index = STEP ? 0 : load_shared(a.tail_index + owner);
     for (int32_t c0 = col_first; c0 < col_end; c0 += kColumns * lanes) {
+        __syncthreads();                         // (`part` is free)
         float sum[kColumns];
         float squares = 0.f;
         float weight[kColumns], state = 0.f, lr = 0.f;
@@ -96,30 +115,34 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
 #pragma unroll
                 for (int p = 0; p < kColumns; ++p) sum[p] += t0 + u * sharers <= last ? v[u][p] : 0.f;
         }
+        if (sharers > 1) {
+#pragma unroll
+            for (int p = 0; p < kColumns; ++p) part[p * kReduceBlock + threadIdx.x] = sum[p];
+            __syncthreads();
+            if (sharer == 0) {
+#pragma unroll
+                for (int g = 1; g < kReduceBlock / kWave; ++g)
+#pragma unroll
+                    for (int p = 0; p < kColumns; ++p) sum[p] += g < sharers ? part[p * kReduceBlock + (g < sharers ? g : 0) * lanes + lane] : 0.f;
+            }
+        }
 #pragma unroll
         for (int p = 0; p < kColumns; ++p) {
             const int32_t c = c0 + p * lanes + lane;
-            if (sharers > 1) {
-                part[threadIdx.x] = sum[p];
-                __syncthreads();
-                if (sharer == 0)
-                    for (int g = 1; g < sharers; ++g) sum[p] += part[g * lanes + lane];
-                __syncthreads();
-            }
             sum[p] *= a.factor;
             if (c < col_end && sharer == 0) squares += sum[p] * sum[p];
         }
         if constexpr (STEP) {
             float rate = lr;
             if (a.state) {
-                part[threadIdx.x] = squares;
+                __syncthreads();                  // (the shares have been read)
+                const float of_wave = group_sum(squares, kWave);
+                if (lane_id() == 0) part[threadIdx.x / kWave] = of_wave;
                 __syncthreads();
-                for (int d = kReduceBlock / 2; d > 0; d >>= 1) {
-                    if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
-                    __syncthreads();
-                }
-                state += part[0] / (float)a.dim;
-                __syncthreads();                  // (all have read both)
+                float all = 0.f;
+#pragma unroll
+                for (int w = 0; w < kReduceBlock / kWave; ++w) all += part[w];
+                state += all / (float)a.dim;
                 if (threadIdx.x == 0) a.state[row] = state;
                 rate = lr / (sqrtf(state) + a.eps);
             }
@@ -150,6 +173,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
     __shared__ uint32_t heads_before[kWaves], heads_here[kWaves], wave_through[kWaves], joins;
     __shared__ Floats<V> shares[NP][kReduceBlock];
+    __shared__ float join_part[kJoinColumns * kReduceBlock];
 
     const int32_t tile_index = (int32_t)(blockIdx.x / (uint32_t)a.col_blocks), block_col = (int32_t)(blockIdx.x % (uint32_t)a.col_blocks);
     const int64_t first = (int64_t)tile_index * a.tile;
@@ -169,12 +193,8 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         row_of_entry[0] = first > 0 ? row_at(a.entries, first - 1) : kNoRow;
         row_of_entry[m + behind + 1] = first + m + behind < a.n ? row_at(a.entries, first + m + behind) : kNoRow;
     }
-    __syncthreads();
-    const int begin = group * per < m ? group * per : m, end = begin + per < m ? begin + per : m;
-    // `index`: runs that begin before the part
-    uint32_t index = 0;
+    uint32_t earlier = 0;                        // runs that begin in the tiles before this: a lane's share of them
     if constexpr (!STEP) {
-        uint32_t earlier = 0, mine = 0;          // in the tiles before this, one lane's share; in this part
         if (a.heads_are == kOfTile) {
             for (int t = threadIdx.x; t < tile_index; t += kReduceBlock) earlier += a.heads[t];
         } else if (a.heads_are == kCountHere) {
@@ -186,6 +206,13 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         } else if (threadIdx.x == 0) {
             earlier = a.heads[tile_index];
         }
+    }
+    __syncthreads();
+    const int begin = group * per < m ? group * per : m, end = begin + per < m ? begin + per : m;
+    // `index`: runs that begin before the part
+    uint32_t index = 0;
+    if constexpr (!STEP) {
+        uint32_t mine = 0;                       // in this part
         for (int k = begin + lane; k < end; k += a.lanes)
             mine += row_of_entry[k + 1] != a.num_rows && row_of_entry[k + 1] != row_of_entry[k];
         for (int d = 1; d < a.lanes; d <<= 1) mine += __shfl_xor(mine, d);
@@ -247,7 +274,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
                     const float g = sum[p][e] * a.factor;
                     if (column[p] < a.dim) squares += g * g;
                 }
-            for (int d = 1; d < a.lanes; d <<= 1) squares += __shfl_xor(squares, d);
+            squares = group_sum(squares, a.lanes);
             state += squares / (float)a.dim;
             if (lane == 0) a.state[row] = state;
             rate = lr / (sqrtf(state) + a.eps);
@@ -263,16 +290,6 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 #pragma unroll
         for (int p = 0; p < NP; ++p)
             if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor, a.past_caches);
-    };
-    auto emit_row = [&](uint32_t row, uint32_t at) {
-        if constexpr (STEP) {
-            Weights w[NP];
-            float state;
-            load_weights(row, w, state);
-            emit_step(row, w, state);
-        } else {
-            emit_grad(row, at);
-        }
     };
     // (unconditional loads, so that all that are asked for are under way at a time: where nothing is wanted, of a row that is in the
     // caches anyway; a lane without columns has the first one)
@@ -341,6 +358,10 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 
     // A chain is the shares of following parts as far as a run goes: first inside every wavefront, from each of its parts to its
     // end, by doubling; the chains from the wavefronts' first parts then go to LDS.
+    const bool had_tail = flags & kTailShare;
+    Weights tail_weights[NP];                    // (of the run that goes on: under way meanwhile)
+    float tail_state = 0.f;
+    if constexpr (STEP) load_weights(had_tail ? row_of_entry[end] : 0, tail_weights, tail_state);
     const int in_wave = kWave / a.lanes, place = group % in_wave;
     Floats<V> chain[NP];
     bool through = flags & kThrough;
@@ -364,7 +385,6 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         if (lane == 0) wave_through[wave] = through;
     }
     // the run that the part leaves unfinished goes on with the next part's chain
-    const bool had_tail = flags & kTailShare;
     bool unfinished = had_tail;
     {
         const bool next = __shfl_down((int)through, a.lanes);
@@ -379,6 +399,10 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         if (adds) unfinished = next;
     }
     __syncthreads();
+    auto emit_tail = [&]() {
+        if constexpr (STEP) emit_step(row_of_entry[end], tail_weights, tail_state);
+        else emit_grad(row_of_entry[end], index - 1);
+    };
     auto follow = [&](Floats<V> (&to)[NP], int w) {      // ... and with those of the wavefronts from w on; whether it leaves the tile
         int until = w;
         while (until < kWaves && wave_through[until]) ++until;
@@ -390,7 +414,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         return until == kWaves;
     };
     if (unfinished) unfinished = follow(sum, wave + 1);
-    if (had_tail && !unfinished) emit_row(row_of_entry[end], index - 1);
+    if (had_tail && !unfinished) emit_tail();
     // the run that came from the tile before
     const bool has_head = group == 0 && (flags & kHeadShare);
     const bool head_goes_on = has_head && through && follow(chain, 1);
@@ -440,7 +464,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
                     else chain[p] += x;
                 }
         }
-        if (unfinished) emit_row(tile_end_row, index - 1);
+        if (unfinished) emit_tail();
         unfinished = false;
     }
     // Shares go to memory by way of LDS, so that neighbouring lanes store neighbouring elements (past the L2s every store is a
@@ -507,7 +531,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         }
         __syncthreads();
         if (!joins) continue;
-        join_run<STEP>(a, part, row, owner, last, col_first, col_first + columns);
+        join_run<STEP>(a, join_part, row, owner, last, col_first, col_first + columns);
         __syncthreads();
     }
 }

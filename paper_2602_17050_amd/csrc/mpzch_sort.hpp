@@ -49,7 +49,12 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
         const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
         before += (r[0] <= row) + (r[1] <= row) + (r[2] <= row) + (r[3] <= row);
     }
-    for (int32_t j = first; j < last; ++j) before += rows[j] < row || (rows[j] == row && j < mine);
+#pragma unroll 4
+    for (int32_t j = first; j < last; j += 4) {
+        const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) before += r[k] < row || (r[k] == row && j + k < mine);
+    }
 #pragma unroll 4
     for (int32_t j = last; j < end; j += 4) {
         const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
