@@ -54,6 +54,10 @@ struct Rows {
 // Results of this many bytes are stored past the caches.  With a kernel behind that reads them, us, through / past: lookups of 8 MB
 // 11.9 / 12.0, 33 MB 23.7 / 23.1, 77 MB 45.0 / 44.4, 180 MB 119.8 / 119.7.
 constexpr int64_t kPastCaches = (int64_t)1 << 24;
+// Gradients of this many bytes are read past the caches, of which the rest of the program keeps more that way: half of the memory-side
+// one, since what a backward pass has just written may still be there.  Sums of 512 MB 298 / 289 us, a step from 256 MB 175 / 168;
+// of 38 MB, which the cache did hold, 62 / 65.
+constexpr int64_t kReadPastCaches = (int64_t)1 << 27;
 
 // scale and dropout of a call
 bool make_mask(float scale, double drop_p, const int64_t *seed, int64_t dim, float *factor, Mask *mask)
@@ -284,6 +288,7 @@ mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, i
     a.col_blocks = p.col_blocks;
     a.grad = (const char *)grad.at;
     a.grad_stride = grad.stride;
+    a.read_past_caches = n * grad.dim * element_bytes(grad.type) >= kReadPastCaches;
     a.tail_index = w.tail_index;
     a.arrived = w.arrived;
     a.head = w.head;
@@ -328,9 +333,8 @@ mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n, const void *rows, in
     a.pieces = div32((uint32_t)(dim / width));
     a.past_caches = n * dim * element_bytes(out_type) >= kPastCaches;
     hipStream_t s = (hipStream_t)stream;
-    int num_cus = 0;
-    TRY(device_cus(&num_cus));
-    const int grid = grid_for(n * a.pieces.d, kBlock * kEmbedPieces, num_cus, 32);
+    const int64_t blocks = ceil_div(n * a.pieces.d, kBlock * kEmbedPieces);
+    const int grid = (int)(blocks < kEmbedBlocks ? blocks : kEmbedBlocks);
     switch (rows_type) {
     case MPZCH_F32: return launch_embed<float>(a, out_type, width, grid, s);
     case MPZCH_BF16: return launch_embed<__bf16>(a, out_type, width, grid, s);

@@ -321,7 +321,24 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             const uint32_t row = row_of_entry[k + 1];
             const bool wanted = row != a.num_rows && row != skipped;
             at[u] = position[wanted ? k : 0];
-            load_grad(at[u], g[u]);
+        }
+        if (a.read_past_caches) {
+            asm volatile("" ::: "memory");       // (or the compiler makes plain loads of both)
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+                    g[u][p].load_past_caches(a.grad + (int64_t)at[u] * a.grad_stride, column[p] < a.dim ? column[p] : 0);
+            asm volatile("" ::: "memory");
+        } else {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) load_grad(at[u], g[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = k0 + u < end ? k0 + u : end - 1;
+            const uint32_t row = row_of_entry[k + 1];
+            const bool wanted = row != a.num_rows && row != skipped;
             if constexpr (STEP) load_weights(wanted && row_of_entry[k + 2] != row ? row : 0, w[u], state[u]);
         }
 #pragma unroll

@@ -16,6 +16,7 @@ struct ReduceArgs {
     int32_t col_blocks;          // workgroups that share out the columns of a tile
     const char *grad;
     int64_t grad_stride;
+    bool read_past_caches;       // grad is loaded non-temporally
     int32_t dim;
     float factor;
     Mask mask;
