@@ -252,7 +252,7 @@ mpzch_status_t sort_slots(const Areas &w, const int64_t *slots, int64_t n, int64
     SortSource src{slots, nullptr, row_mod(num_rows), n, 32, 0};
     if (n <= kRankMax) {
         *out = w.entries[0];
-        return launch(k_sort_rank, (int)ceil_div(n, kWave), kSortBlock, s, slots, src.mod, (int32_t)n, w.entries[0]);
+        return launch(k_sort_rank, (int)ceil_div(n, kRanked), kSortBlock, s, slots, src.mod, (int32_t)n, w.entries[0]);
     }
     const SortPlan p = sort_plan(n, num_rows);
     src.bits = p.bits;

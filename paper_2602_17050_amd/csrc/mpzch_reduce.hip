@@ -47,6 +47,16 @@ __device__ __forceinline__ float group_sum(float x, int lanes)
     return x;
 }
 
+[[maybe_unused]] __device__ __forceinline__ uint32_t wave_sum(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true);
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
 // how many of x(0) .. x(count - 1), ascending, are below v (or, with EQUAL, not above it): a wavefront looks at 64 of them at a time
 template <bool EQUAL, typename X>
 __device__ __forceinline__ int32_t wave_search(int32_t count, uint32_t v, X x)
@@ -171,7 +181,8 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     constexpr bool STEP = WB != 0;
     constexpr int kWaves = kReduceBlock / kWave;
     __shared__ uint32_t row_of_entry[kReduceTile + kBehind + 2], position[kReduceTile + kBehind];
-    __shared__ uint32_t heads_before[kWaves], heads_here[kWaves], wave_through[kWaves], joins;
+    __shared__ uint32_t heads_before[kWaves], wave_through[kWaves], joins;
+    __shared__ uint64_t run_begins[(kReduceTile + kBehind) / kWave];
     __shared__ Floats<V> shares[NP][kReduceBlock];
     __shared__ float join_part[kJoinColumns * kReduceBlock];
 
@@ -183,10 +194,16 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     const int groups = kReduceBlock / a.lanes, per = a.tile / groups;
     const int group = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes, wave = threadIdx.x / kWave;
 
-    // the tile's entries and the next ones, the row before them and the one behind
+    // the tile's entries and the next ones, the row before them and the one behind; for a gradient, where runs begin, 64 entries a word
     for (int k = threadIdx.x; k < m + behind; k += kReduceBlock) {
         const uint64_t e = a.entries[first + k];
-        row_of_entry[k + 1] = (uint32_t)(e >> 32);
+        const uint32_t row = (uint32_t)(e >> 32);
+        if constexpr (!STEP) {
+            const uint32_t before = first + k > 0 ? row_at(a.entries, first + k - 1) : kNoRow;
+            const uint64_t begins = __ballot(k < m && row != a.num_rows && row != before);
+            if (lane_id() == 0) run_begins[k / kWave] = begins;
+        }
+        row_of_entry[k + 1] = row;
         position[k] = (uint32_t)e;
     }
     if (threadIdx.x == 0) {
@@ -207,36 +224,26 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             earlier = a.heads[tile_index];
         }
     }
+    if constexpr (!STEP) {
+        earlier = wave_sum(earlier);
+        if (lane_id() == 0) heads_before[wave] = earlier;
+    }
     __syncthreads();
     const int begin = group * per < m ? group * per : m, end = begin + per < m ? begin + per : m;
     // `index`: runs that begin before the part
     uint32_t index = 0;
     if constexpr (!STEP) {
-        uint32_t mine = 0;                       // in this part
-        for (int k = begin + lane; k < end; k += a.lanes)
-            mine += row_of_entry[k + 1] != a.num_rows && row_of_entry[k + 1] != row_of_entry[k];
-        for (int d = 1; d < a.lanes; d <<= 1) mine += __shfl_xor(mine, d);
-        uint32_t upto = mine;                    // of the wavefront's parts
-        for (int d = a.lanes; d < kWave; d <<= 1) {
-            const uint32_t x = __shfl_up(upto, d);
-            if (lane_id() >= d) upto += x;
-        }
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) earlier += __shfl_xor(earlier, d);
-        if (lane_id() == kWave - 1) {
-            heads_before[wave] = earlier;
-            heads_here[wave] = upto;
+        for (int w = 0; w < kWaves; ++w) index += heads_before[w];
+        const bool counts = blockIdx.x == gridDim.x - 1 && threadIdx.x == 0;
+        if (counts) {
+            uint32_t all = 0;
+            for (int k = 0; k < m; k += kWave) all += (uint32_t)__popcll(run_begins[k / kWave]);
+            *a.out_count = (int64_t)index + all;
         }
-        __syncthreads();
-        uint32_t all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            index += heads_before[w];
-            if (w < wave) index += heads_here[w];
-            all += heads_here[w];
-        }
-        if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *a.out_count = (int64_t)index + all;
-        index += upto - mine;
+#pragma unroll 4
+        for (int k = 0; k < begin / kWave; ++k) index += (uint32_t)__popcll(run_begins[k]);
+        if (begin % kWave) index += (uint32_t)__popcll(run_begins[begin / kWave] & ((1ull << begin % kWave) - 1));
     }
     // what is left out: padding, and the rest of a run that an earlier tile has finished
     const uint32_t tile_end_row = m > 0 ? row_of_entry[m] : kNoRow;

@@ -25,25 +25,26 @@ __device__ __forceinline__ uint64_t sort_entry(const SortSource &s, int64_t i)
     else return s.entries[i];
 }
 
-// Short batches: an entry's place is the number of entries before it, counted over all of them by 64 lanes with an entry each
-// and 16 wavefronts with a part of the batch each.  n^2 comparisons, but one launch.
+// Short batches: an entry's place is the number of entries before it.  A workgroup counts for 32 entries, an entry in two lanes of each
+// of its 16 wavefronts, which have a 32nd of the batch each.  n^2 comparisons, but one launch, and all compute units share them.
 constexpr int kRankMax = 8192;
+constexpr int kRanked = 32, kRankParts = kSortBlock / kRanked;
 __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, RowMod mod, int32_t n, uint64_t *out)
 {
     __shared__ __align__(16) uint32_t rows[kRankMax];
-    __shared__ uint32_t place[kWave];
+    __shared__ uint32_t place[kRanked];
     const int32_t whole = (n + 3) / 4 * 4;
     for (int32_t i = threadIdx.x; i < whole; i += kSortBlock) rows[i] = i < n ? sort_row(mod, slots[i]) : ~0u;
-    if (threadIdx.x < kWave) place[threadIdx.x] = 0;
+    if (threadIdx.x < kRanked) place[threadIdx.x] = 0;
     __syncthreads();
-    const int32_t block = (int32_t)blockIdx.x * kWave, mine = block + lane_id();
+    const int32_t block = (int32_t)blockIdx.x * kRanked, mine = block + (int32_t)threadIdx.x % kRanked;
     const uint32_t row = rows[mine < n ? mine : n - 1];
-    const int32_t wave = threadIdx.x / kWave, share = (whole / 4 + kSortWaves - 1) / kSortWaves * 4;
-    const int32_t begin = wave * share < whole ? wave * share : whole, end = begin + share < whole ? begin + share : whole;
+    const int32_t part = threadIdx.x / kRanked, share = (whole / 4 + kRankParts - 1) / kRankParts * 4;
+    const int32_t begin = part * share < whole ? part * share : whole, end = begin + share < whole ? begin + share : whole;
     uint32_t before = 0;
-    auto upto = [&](int32_t at, int32_t from, int32_t to) { return at < from ? from : at > to ? to : at; };
-    // entries before the 64 of this workgroup, among them, behind them
-    const int32_t first = upto(block, begin, end), last = upto(block + kWave, begin, end);
+    auto upto = [&](int32_t at) { return at < begin ? begin : at > end ? end : at; };
+    // entries before the 32 of this workgroup, among them, behind them (all borders are multiples of four)
+    const int32_t first = upto(block), last = upto(block + kRanked);
 #pragma unroll 4
     for (int32_t j = begin; j < first; j += 4) {
         const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
@@ -60,9 +61,9 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
         const u32x4 r = *reinterpret_cast<const u32x4 *>(rows + j);
         before += (r[0] < row) + (r[1] < row) + (r[2] < row) + (r[3] < row);
     }
-    atomicAdd(&place[lane_id()], before);
+    atomicAdd(&place[threadIdx.x % kRanked], before);
     __syncthreads();
-    if (threadIdx.x < kWave && mine < n) out[place[threadIdx.x]] = (uint64_t)row << 32 | (uint32_t)mine;
+    if (threadIdx.x < kRanked && mine < n) out[place[threadIdx.x]] = (uint64_t)row << 32 | (uint32_t)mine;
 }
 
 // Longer ones: a radix sort, least significant digit first, each pass stable, so that the positions of a row stay ascending.
