@@ -25,10 +25,10 @@ __device__ __forceinline__ uint64_t sort_entry(const SortSource &s, int64_t i)
     else return s.entries[i];
 }
 
-// Short batches: an entry's place is the number of entries before it.  A workgroup counts for 32 entries, an entry in two lanes of each
-// of its 16 wavefronts, which have a 32nd of the batch each.  n^2 comparisons, but one launch, and all compute units share them.
+// Short batches: an entry's place is the number of entries before it.  A workgroup counts for 16 entries, an entry in four lanes of each
+// of its 16 wavefronts, which have a 64th of the batch each.  n^2 comparisons, but one launch, and all compute units share them.
 constexpr int kRankMax = 8192;
-constexpr int kRanked = 32, kRankParts = kSortBlock / kRanked;
+constexpr int kRanked = 16, kRankParts = kSortBlock / kRanked;
 __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, RowMod mod, int32_t n, uint64_t *out)
 {
     __shared__ __align__(16) uint32_t rows[kRankMax];
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
     const int32_t begin = part * share < whole ? part * share : whole, end = begin + share < whole ? begin + share : whole;
     uint32_t before = 0;
     auto upto = [&](int32_t at) { return at < begin ? begin : at > end ? end : at; };
-    // entries before the 32 of this workgroup, among them, behind them (all borders are multiples of four)
+    // entries before the 16 of this workgroup, among them, behind them (all borders are multiples of four)
     const int32_t first = upto(block), last = upto(block + kRanked);
 #pragma unroll 4
     for (int32_t j = begin; j < first; j += 4) {
@@ -68,7 +68,9 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, 
 
 // Longer ones: a radix sort, least significant digit first, each pass stable, so that the positions of a row stay ascending.
 // A pass counts the digits of every tile (k_sort_hist), adds up what earlier tiles hold (k_sort_scan; where there are few
-// tiles, k_sort_scatter itself) and moves the entries (k_sort_scatter).
+// tiles, k_sort_scatter itself) and moves the entries (k_sort_scatter).  The last of these could count the next pass's digits as
+// it goes, with atomics on the counts of the tiles that it moves entries to, and save a launch: a step of 65 536 positions
+// 40 -> 57 us, of 1 M 174 -> 383.
 // Digits of up to kWideBits bits where passes are few launches after all, of kNarrowBits where there are many entries to move: the
 // more digits, the shorter the stretches that a tile stores side by side.
 constexpr int kWideBits = 11, kNarrowBits = 9, kLeastBits = 6;
