@@ -426,7 +426,7 @@ mpzch_status_t mpzch_lookup_jagged(mpzch_group_t *g, const int64_t *const *ident
  *                       state == NULL (SGD)             w[r, :] -= lr * G[r, :]
  *                       else     (row-wise Adagrad)     state[r] += mean_j G[r, j]^2
  *                                                       w[r, :] -= lr * G[r, :] / (sqrt(state[r]) + eps)
- * A negative slot is padding: its output row is zeros, its gradient row is not read, it names no row.
+ * A negative slot is padding: its output row is zeros, its gradient row does not count, it names no row.
  * What is dropped or padded is zero whatever the row or gradient holds there (infinities and NaN among it).
  *
  * Dropout.  The mask is not stored: gradient and step draw it again from the same seed.  With
@@ -444,7 +444,7 @@ mpzch_status_t mpzch_lookup_jagged(mpzch_group_t *g, const int64_t *const *ident
  *            8 (4 with 32-bit elements) on 16-byte boundaries is the fastest.
  * scale      finite;  drop_p in [0, 1];  seed [dev] uint64[1], may be NULL where T is 0
  * Products and sums are formed in 32-bit floats and rounded once, to nearest, to the type of the result; the order of a
- * sum is determined by n, dim, the types and the positions of the row: the same call gives the same bits.
+ * sum is determined by n, dim, the types, the tensors' alignment and the slots: the same call gives the same bits.
  * No output may overlap an input (of a step: rows and state are updated in place).
  */
 typedef enum { MPZCH_F32 = 0, MPZCH_BF16 = 1, MPZCH_F16 = 2 } mpzch_type_t;
@@ -462,8 +462,9 @@ mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n,
  * time, captured ones included (two graphs that share a handle must not run side by side).  The scratch is allocated by
  * mpzch_embed_reserve, or grown by the first call that needs more (which synchronises the device, and must not be
  * captured), on the device that is current then; a call with another device current is answered with INVALID_ARG.
- * 16 bytes per position of max_n, and 8 per element of max_dim for each 64 positions up to 2 048 times (beyond
- * 4 194 304 positions for each 2 048).  Errors: INVALID_ARG, ALLOC.
+ * Growth replaces the scratch: graphs that were captured before hold the old one and must not be replayed.
+ * 17 bytes per position of max_n, 8 per element of max_dim for each 32 positions up to 512 times (beyond 1 048 576
+ * positions for each 2 048), and a megabyte.  Errors: INVALID_ARG, ALLOC.
  * With enough scratch the calls below only launch kernels on the given stream, whatever the slots, and may be captured.
  */
 typedef struct mpzch_embed_s mpzch_embed_t;

@@ -10,19 +10,23 @@ namespace {
 // A run is the entries of one row.  A workgroup has a tile of neighbouring entries, a group of lanes in it (a power of two of
 // them, V * NP elements of the row for each) a part of the tile.  What a group knows of a run:
 //   it begins and ends in the part   the group emits its sum
-//   it began before                  the part's share goes to LDS, and whether the run goes on behind the part
-//   it goes on behind                the group in whose part it begins adds the following groups' shares, in their order
-// A run that goes on behind the tile for kBehind entries at most is finished there by the group that has its sum, and the
-// following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to write one is
-// found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and the run's
-// place alone determine: who is last does not change it.
+//   it began before                  the part has a share of it; it may go through the part
+//   it goes on behind                the group in whose part it begins adds the shares of the parts that it goes through
+// A run that goes on behind the tile for kBehind entries at most is finished there, by all groups of the workgroup in which it
+// is, and the following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to
+// write one is found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and
+// the run's place alone determine: who is last does not change it.
+//
+// Bound by memory where batches are long: every gradient row is read once, 256 bytes and more at a random place.  2 M positions
+// of 128 bf16 elements (799 MB to move) take this kernel 190 us (4.2 TB/s; a copy 4.8), a step of 1 M (394 MB) 116.  By round
+// trips where they are short: entries, gradients and weights, shares.  65 536 positions with a step (20 MB) 16 us, 1 024 7.
 constexpr int kBehind = 128;
 constexpr uint32_t kNoRow = ~0u;
 constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part
 
 // Shares are read by a workgroup that may run on another die, with an L2 of its own: they are stored and loaded as atomics of the
 // whole device, which go past the L2s one by one.  (A fence of the device instead writes the whole L2 back, the other workgroups'
-// outputs with it.)
+// outputs with it: gradient of 2 M positions 336 -> 535 us.)
 template <typename T>
 __device__ __forceinline__ void store_shared(T *to, T v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename T>
@@ -314,6 +318,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         }
     };
 
+    // entries under way at a time: with 8 a step of 1 M positions took 247 instead of 182 us, with 2 192 (registers, wavefronts)
     constexpr int kAhead = NP > 1 ? 2 : 4;
     uint32_t flags = 0;
     bool from_before = begin < end && row_of_entry[begin] == row_of_entry[begin + 1];

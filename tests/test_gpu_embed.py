@@ -276,6 +276,61 @@ def test_embed_grad_of_a_long_batch(handle):
     mp.mpzch_embed_destroy(h)
 
 
+RUNS = [1, 1, 2, 3, 5, 31, 32, 33, 63, 64, 65, 127, 128, 129, 130, 160, 191, 192, 193, 255, 256, 257, 258, 300, 383, 384, 385, 511, 512, 513,
+        640, 1000, 1024, 1025, 2047, 2048, 2049, 2175, 2176, 2177, 2178, 4000]
+
+
+@pytest.mark.parametrize("dim,dtype", [(1, F32), (2, BF16), (16, F32), (64, BF16), (130, F32), (512, BF16), (513, F32), (1024, BF16), (2056, BF16)])
+@pytest.mark.parametrize("order", ["up", "down", "mixed", "short"])
+def test_sums_of_runs_of_every_length(handle, dim, dtype, order):
+    """Runs that end and begin at, before and behind the borders of parts, tiles and what lies behind them; sums of small whole
+    numbers are exact, so the results of gradient and step are, too."""
+    rng = np.random.Generator(np.random.Philox(key=dim * 10 + len(order)))
+    lengths = {"up": RUNS, "down": RUNS[::-1], "mixed": list(rng.permutation(RUNS + [1] * 300 + [2] * 100)), "short": RUNS[:16] * 3}[order]
+    if dim > 600:
+        lengths = [x for x in lengths if x < 1100]
+    slots_np = np.repeat(np.arange(len(lengths)) * 3 + 1, lengths).astype(np.int64)
+    n, num_rows = len(slots_np), 3 * len(lengths) + 2
+    slots_np = slots_np[rng.permutation(n)]
+    grad_np = rng.integers(-4, 5, size=(n, dim)).astype(np.float32)
+    grad = torch.from_numpy(grad_np).cuda().to(dtype)
+    say("runs", n, num_rows, dim, dtype, order)
+    got_slots, got_rows, count = run_grad(handle, slots_np, grad, num_rows, F32, 1.0, 0.0, 0)
+    named, total, _, _ = ref.sums(slots_np, grad_np, num_rows, 1.0, 0.0, 0)
+    assert count == len(named) and np.array_equal(got_slots[:count], named)
+    assert np.array_equal(f64(got_rows)[:count], total) and (f64(got_rows)[count:] == -77).all()
+    if dim > 1024:
+        return
+    rows = torch.zeros(num_rows, dim, device="cuda")             # SGD with a rate of 1 / 2 from zero: -total / 2
+    mp.mpzch_embed_step(handle, torch.from_numpy(slots_np).cuda(), grad, rows, None, torch.full((1,), 0.5, device="cuda"))
+    want = np.zeros((num_rows, dim))
+    want[named] = -0.5 * total
+    assert np.array_equal(f64(rows), want)
+
+
+@pytest.mark.parametrize("n,num_rows", [(8192, 100), (8193, 100), (65_536, 70_000), (65_537, 70_000), (70_001, (1 << 32) - 2),
+                                        (524_288, 1 << 20), (524_289, 1 << 20), (1_048_576, 33), (1_048_577, 33_000_000), (2_100_000, 7)])
+def test_gradients_of_every_way_to_sort(handle, n, num_rows):
+    """Sizes on both sides of where another sort takes over; whole numbers again."""
+    rng = np.random.Generator(np.random.Philox(key=n))
+    slots_np = draw_slots(rng, n, num_rows, "zipf")
+    grad_np = rng.integers(-8, 9, size=(n, 2)).astype(np.float32)
+    say("sort", n, num_rows)
+    got_slots, got_rows, count = run_grad(handle, slots_np, torch.from_numpy(grad_np).cuda(), num_rows, F32, 1.0, 0.0, 0)
+    named, total, _, _ = ref.sums(slots_np, grad_np, num_rows, 1.0, 0.0, 0)
+    assert count == len(named) and np.array_equal(got_slots[:count], named)
+    assert np.array_equal(f64(got_rows)[:count], total)
+
+
+def test_scratch_grows_and_keeps_what_it_had_room_for():
+    """A handle that is used before anything is reserved, then for longer batches and rows, then for short ones again."""
+    h = mp.mpzch_embed_create()
+    rng = np.random.Generator(np.random.Philox(key=21))
+    for n, dim in ((10, 4), (5000, 4), (100, 700), (70_000, 12), (3, 3000), (70_000, 16), (1, 1)):
+        check_grad(h, draw_slots(rng, n, 50, "zipf"), tensor2d(rng, n, dim, F32), 50, F32, 1.0, 0.0, 0)
+    mp.mpzch_embed_destroy(h)
+
+
 def test_embed_grad_against_differences(handle):
     """The derivative of <c, embed(rows)> in the direction d is <G, d>: the lookup is linear, so the difference quotient over a
     step of 1 has only the roundings of the two lookups: 2 (2 u) sum |c| f (|w| + |d|), and the gradient's."""
