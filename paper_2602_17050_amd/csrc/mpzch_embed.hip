@@ -40,16 +40,15 @@ struct Rows {
         const int64_t e = element_bytes(type);
         return at && type_ok(type) && stride >= dim * e && stride % e == 0 && (uintptr_t)at % e == 0;
     }
-    // the most elements, of 8, 4, 2, 1, that every row holds whole numbers of and that are aligned in memory (16 bytes will do)
-    int width() const
-    {
-        for (int v = 8; v > 1; v /= 2) {
-            const int64_t bytes = v * element_bytes(type), need = bytes < 16 ? bytes : 16;
-            if (dim % v == 0 && (uintptr_t)at % need == 0 && stride % need == 0) return v;
-        }
-        return 1;
-    }
 };
+
+// elements of a piece: 16 bytes of the wider of two tensors, or what a short row has
+int piece_width(int64_t dim, int32_t type, int32_t other)
+{
+    int width = type == MPZCH_F32 || other == MPZCH_F32 ? 4 : 8;
+    while (width > dim) width /= 2;
+    return width;
+}
 
 // Results of this many bytes are stored past the caches.  With a kernel behind that reads them, us, through / past: lookups of 8 MB
 // 11.9 / 12.0, 33 MB 23.7 / 23.1, 77 MB 45.0 / 44.4, 180 MB 119.8 / 119.7.
@@ -110,14 +109,12 @@ constexpr int64_t kTilesAdded = 2048;        // up to which a workgroup itself a
 struct ReducePlan {
     int lanes, pieces, col_blocks, tile, tiles;      // pieces: of a lane, as compiled
 };
-// pieces of a row that a lane has where there are more of them than lanes
-int many_pieces(int width) { return 16 / width; }
 ReducePlan reduce_plan(int64_t n, int64_t dim, int width)
 {
     ReducePlan p;
-    const int64_t pieces = dim / width;
+    const int64_t pieces = ceil_div(dim, width);
     p.lanes = pieces < kWave ? pow2_at_least(pieces) : kWave;
-    p.pieces = pieces <= kWave ? 1 : many_pieces(width);
+    p.pieces = pieces <= kWave ? 1 : 16 / width;
     p.col_blocks = (int)ceil_div(pieces, (int64_t)p.lanes * p.pieces);
     const int groups = kReduceBlock / p.lanes;
     int64_t per = ceil_div(n * p.lanes * p.col_blocks, kWave * kReduceWaves);
@@ -270,8 +267,8 @@ mpzch_status_t sort_slots(const Areas &w, const int64_t *slots, int64_t n, int64
 
 // Everything behind the argument checks.  `a` holds what the caller gave.
 template <bool STEP>
-mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows, const Rows &grad, int width,
-                            ReduceArgs a, hipStream_t s)
+mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows, const Rows &grad, ReduceArgs a,
+                            hipStream_t s)
 {
     TRY(ensure(h, n, grad.dim));
     Areas w;
@@ -279,7 +276,7 @@ mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, i
     if (n > 0) TRY(sort_slots(w, slots, n, num_rows, &a.entries, s));
     else a.entries = w.entries[0];
 
-    if (width == 8 && grad.type == MPZCH_F32) width = 4;
+    const int width = piece_width(grad.dim, grad.type, grad.type);
     const ReducePlan p = reduce_plan(n, grad.dim, width);
     a.n = n;
     a.num_rows = (uint32_t)num_rows;
@@ -323,8 +320,7 @@ mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n, const void *rows, in
     if (!make_mask(scale, drop_p, seed, dim, &a.factor, &a.mask)) return MPZCH_ERR_INVALID_ARG;
     if (n == 0 && type_ok(rows_type) && type_ok(out_type)) return MPZCH_OK;
     if (!slots || !in.ok() || !to.ok()) return MPZCH_ERR_INVALID_ARG;
-    int width = in.width() < to.width() ? in.width() : to.width();
-    if (width == 8 && (rows_type == MPZCH_F32 || out_type == MPZCH_F32)) width = 4;
+    const int width = piece_width(dim, rows_type, out_type);
     a.slots = slots;
     a.n = n;
     a.rows = (const char *)rows;
@@ -332,7 +328,8 @@ mpzch_status_t mpzch_embed(const int64_t *slots, int64_t n, const void *rows, in
     a.row_stride = row_stride_bytes;
     a.out = (char *)out;
     a.out_stride = out_stride_bytes;
-    a.pieces = div32((uint32_t)(dim / width));
+    a.dim = (int32_t)dim;
+    a.pieces = div32((uint32_t)ceil_div(dim, width));
     a.past_caches = n * dim * element_bytes(out_type) >= kPastCaches;
     hipStream_t s = (hipStream_t)stream;
     const int64_t blocks = ceil_div(n * a.pieces.d, kBlock * kEmbedPieces);
@@ -385,14 +382,13 @@ mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t 
     const Rows to{out_rows, out_type, dim, dim * element_bytes(out_type)};
     if (n > 0 && (!slots || !g.ok())) return MPZCH_ERR_INVALID_ARG;
     if (out_cap > 0 && (!out_slots || !to.ok())) return MPZCH_ERR_INVALID_ARG;
-    const int width = out_cap > 0 && to.width() < g.width() ? to.width() : g.width();
     a.out_slots = out_slots;
     a.out_count = out_count;
     a.out_rows = (char *)out_rows;
     a.cap = out_cap;
     a.past_caches = (n < out_cap ? n : out_cap) * dim * element_bytes(out_type) >= kPastCaches;
     a.type = out_type;
-    return run_gradient<false>(h, slots, n, num_rows, g, width, a, (hipStream_t)stream);
+    return run_gradient<false>(h, slots, n, num_rows, g, a, (hipStream_t)stream);
 }
 
 mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t n,
@@ -418,7 +414,7 @@ mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t 
     a.state = state;
     a.lr = lr;
     a.eps = eps;
-    return run_gradient<true>(h, slots, n, num_rows, g, g.width() < w.width() ? g.width() : w.width(), a, (hipStream_t)stream);
+    return run_gradient<true>(h, slots, n, num_rows, g, a, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -15,10 +15,12 @@
 
 namespace mpzch {
 
-// V neighbouring elements as they lie in memory; aligned to their size, to 16 bytes at most
+// V neighbouring elements as they lie in memory, aligned as one element: rows of any length and tensors that begin anywhere are
+// read with the same wide loads.  (The last piece of a row whose length is no multiple of V is moved back to the row's last V
+// elements: what two lanes have of it is the same.)
 template <typename E, int V>
 struct PackOf {
-    typedef E type __attribute__((ext_vector_type(V), aligned(V * sizeof(E) < 16 ? V * sizeof(E) : 16)));
+    typedef E type __attribute__((ext_vector_type(V), aligned(sizeof(E))));
 };
 template <typename E, int V>
 using Pack = typename PackOf<E, V>::type;
@@ -99,19 +101,25 @@ struct Mask {
     int32_t words;               // ceil(dim / 4)
 };
 
-// v with the dropped ones of the elements j0 .. j0 + V of position i at zero (j0 a multiple of V)
+// v with the dropped ones of the elements j0 .. j0 + V of position i at zero
 template <int V>
 __device__ __forceinline__ Floats<V> masked(Floats<V> v, uint64_t seed, const Mask &m, int64_t i, int32_t j0)
 {
-    const uint64_t word = (uint64_t)i * (uint64_t)m.words + (uint32_t)(j0 >> 2);
+    const uint64_t first = seed + ((uint64_t)i * (uint64_t)m.words + (uint32_t)(j0 >> 2)) * kGolden;
+    const int shift = 16 * (j0 & 3);
+    constexpr int kWords = (V + 3) / 4;
+    uint64_t draws[kWords];
 #pragma unroll
-    for (int w = 0; w < (V + 3) / 4; ++w) {
-        uint64_t draws = mix64(seed + (word + w) * kGolden);
-        if constexpr (V < 4) draws >>= 16 * (j0 & 3);
+    for (int w = 0; w < kWords; ++w) draws[w] = mix64(first + w * kGolden);
+    if (shift) {                                 // a piece that begins inside a word goes on in the next one
+        uint64_t next = 0;
+        if (shift + 16 * V > 64 * kWords) next = mix64(first + kWords * kGolden);
 #pragma unroll
-        for (int e = 0; e < (V < 4 ? V : 4); ++e)
-            if ((uint32_t)(draws >> (16 * e) & 0xFFFF) < m.threshold) v[4 * w + e] = 0.f;
+        for (int w = 0; w < kWords; ++w) draws[w] = draws[w] >> shift | (w + 1 < kWords ? draws[w + 1 < kWords ? w + 1 : 0] : next) << (64 - shift);
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if ((uint32_t)(draws[e / 4] >> (16 * (e % 4)) & 0xFFFF) < m.threshold) v[e] = 0.f;
     return v;
 }
 
@@ -145,6 +153,7 @@ struct EmbedArgs {
     int64_t row_stride;
     char *out;
     int64_t out_stride;
+    int32_t dim;
     Div32 pieces;                // of a row
     float factor;
     Mask mask;
@@ -162,26 +171,28 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a)
     const uint64_t seed = DROP ? *a.mask.seed : 0;
     for (int64_t i = (int64_t)blockIdx.x * kBlock * kEmbedPieces + threadIdx.x; i - threadIdx.x < total; i += turn) {
         int64_t k[kEmbedPieces], slot[kEmbedPieces];
-        uint32_t c[kEmbedPieces];
+        int32_t column[kEmbedPieces];
         Raw<sizeof(TI), V> v[kEmbedPieces];
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
-            k[u] = k0 + divided(a.pieces, c0 + u * kBlock + threadIdx.x, &c[u]);
+            uint32_t c;
+            k[u] = k0 + divided(a.pieces, c0 + u * kBlock + threadIdx.x, &c);
+            column[u] = (int32_t)c * V < a.dim - V ? (int32_t)c * V : a.dim - V;
             slot[u] = i + u * kBlock < total ? a.slots[k[u]] : -1;
         }
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
             // (padding: the first row, in the caches)
             const int64_t row = slot[u] >= 0 ? row_of(a.mod, slot[u]) : 0;
-            v[u].load(a.rows + row * a.row_stride, c[u] * V);
+            v[u].load(a.rows + row * a.row_stride, column[u]);
         }
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
             if (i + u * kBlock >= total) continue;
             Floats<V> x = v[u].floats(std::is_same_v<TI, __bf16> ? kBf16 : kF16) * a.factor;
-            if constexpr (DROP) x = masked<V>(x, seed, a.mask, k[u], (int32_t)(c[u] * V));
+            if constexpr (DROP) x = masked<V>(x, seed, a.mask, k[u], column[u]);
             if (slot[u] < 0) x = Floats<V>(0.f);
-            store_floats<TO, V>(a.out + k[u] * a.out_stride + (int64_t)c[u] * (V * sizeof(TO)), x, a.past_caches);
+            store_floats<TO, V>(a.out + k[u] * a.out_stride + (int64_t)column[u] * sizeof(TO), x, a.past_caches);
         }
         k0 += dk;
         c0 += dc;

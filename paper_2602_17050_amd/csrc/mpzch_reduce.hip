@@ -258,9 +258,14 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     const bool leaves = m > 0 && row_of_entry[m + 1] == tile_end_row && tile_end_row != a.num_rows && tile_end_row != skipped;
     const bool long_run = leaves && row_of_entry[m + behind + 1] == tile_end_row;      // further than kBehind behind the tile
 
+    // where a piece would begin, and where it does (a.dim: none)
+    const auto piece_of = [&](int p) { return ((block_col * NP + p) * a.lanes + lane) * V; };
     int32_t column[NP];
 #pragma unroll
-    for (int p = 0; p < NP; ++p) column[p] = ((block_col * NP + p) * a.lanes + lane) * V;
+    for (int p = 0; p < NP; ++p) {
+        const int32_t piece = piece_of(p);
+        column[p] = piece < a.dim ? (piece < a.dim - V ? piece : a.dim - V) : a.dim;
+    }
     const uint64_t seed = a.mask.threshold ? *a.mask.seed : 0;
     const float lr = STEP ? *a.lr : 0.f;
     Floats<V> sum[NP];
@@ -278,13 +283,23 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         float rate = lr;
         if (a.state) {
             float squares = 0.f;
+            if (a.dim % V == 0) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+                for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float g = sum[p][e] * a.factor;
-                    if (column[p] < a.dim) squares += g * g;
-                }
+                    for (int e = 0; e < V; ++e) {
+                        const float g = sum[p][e] * a.factor;
+                        if (column[p] < a.dim) squares += g * g;
+                    }
+            } else {                             // (elements that another lane has, too, count once)
+#pragma unroll
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float g = sum[p][e] * a.factor;
+                        if (column[p] < a.dim && column[p] + e >= piece_of(p)) squares += g * g;
+                    }
+            }
             squares = group_sum(squares, a.lanes);
             state += squares / (float)a.dim;
             if (lane == 0) a.state[row] = state;
@@ -509,7 +524,8 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int e = 0; e < V; ++e) to[(p * a.lanes + lane) * V + e] = v[p][e];
+            for (int e = 0; e < V; ++e)
+                if (column[p] < a.dim && column[p] + e >= piece_of(p)) to[column[p] + e - col_first] = v[p][e];
     };
     if (unfinished) {
         keep(part, sum);
@@ -574,8 +590,8 @@ mpzch_status_t launch_reduce(const ReduceArgs &a, int width, int pieces, int gri
             return pieces == 1 ? launch(k_reduce<TG, 8, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 8, 2, WB>, grid, kReduceBlock, s, a);
         return MPZCH_ERR_UNSUPPORTED;
     case 4: return pieces == 1 ? launch(k_reduce<TG, 4, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 4, 4, WB>, grid, kReduceBlock, s, a);
-    case 2: return pieces == 1 ? launch(k_reduce<TG, 2, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 2, 8, WB>, grid, kReduceBlock, s, a);
-    default: return pieces == 1 ? launch(k_reduce<TG, 1, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 1, 16, WB>, grid, kReduceBlock, s, a);
+    case 2: return launch(k_reduce<TG, 2, 1, WB>, grid, kReduceBlock, s, a);       // (rows of three elements, or two)
+    default: return launch(k_reduce<TG, 1, 1, WB>, grid, kReduceBlock, s, a);
     }
 }
 template <int WB>
