@@ -98,12 +98,14 @@ mpzch_status_t launch_embed(const EmbedArgs &a, int32_t out_type, int width, int
 }
 
 // ---- gradient -------------------------------------------------------------------------------
-// How the sums are shared out: kReduceWaves wavefronts or more, but no part of a tile shorter than kPartMin entries and no
-// tile longer than kReduceTile.  us by wavefronts (2 048, 4 096, 8 192): gradient of 300 007 positions 67 62 68, steps of 1 M 176 175
-// 182, of 16 384 positions of 1 024 elements 37.3 36.9 36.7; by the shortest part (2, 4, 8): a step of 65 536 39.1 39.2 44.8, of
-// 16 384 50 42 37 (with four entries under way there; with two 36.9).
+// How the sums are shared out: kReduceWaves wavefronts or more, but no part of a tile shorter than kPartMin entries (or, where
+// the groups are many, no tile shorter than kTileMin) and no tile longer than kReduceTile.  us by wavefronts (2 048, 4 096,
+// 8 192): gradient of 300 007 positions 67 62 68, steps of 1 M 176 175 182, of 16 384 positions of 1 024 elements 37.3 36.9 36.7;
+// by the shortest part (2, 4, 8): a step of 65 536 39.1 39.2 44.8, of 16 384 50 42 37 (with four entries under way there; with
+// two 36.9); without kTileMin / with it: steps of 1 024 and 4 000 positions of 16 elements 11.1 / 10.5 and 16.7 / 15.9, of 20 000 of
+// 64 34.0 / 31.6, a gradient of 20 011 of 50 33.2 / 31.1.
 constexpr int64_t kReduceWaves = 4096;
-constexpr int kPartMin = 4;
+constexpr int kPartMin = 4, kTileMin = 128;
 constexpr int64_t kTilesAdded = 2048;        // up to which a workgroup itself adds up the heads of the tiles before its own
 
 struct ReducePlan {
@@ -118,7 +120,8 @@ ReducePlan reduce_plan(int64_t n, int64_t dim, int width)
     p.col_blocks = (int)ceil_div(pieces, (int64_t)p.lanes * p.pieces);
     const int groups = kReduceBlock / p.lanes;
     int64_t per = ceil_div(n * p.lanes * p.col_blocks, kWave * kReduceWaves);
-    if (per < kPartMin) per = kPartMin;
+    const int least = groups * kPartMin <= kTileMin ? kPartMin : groups < kTileMin ? kTileMin / groups : 1;
+    if (per < least) per = least;
     if (per > kReduceTile / groups) per = kReduceTile / groups;
     p.tile = (int)per * groups;
     p.tiles = n > 0 ? (int)ceil_div(n, p.tile) : 1;
