@@ -99,6 +99,7 @@ struct Mask {
     const uint64_t *seed;
     uint32_t threshold;          // T; 0: no dropout
     int32_t words;               // ceil(dim / 4)
+    int32_t ragged;              // whether pieces may begin inside a word: dim is no multiple of 4
 };
 
 // v with the dropped ones of the elements j0 .. j0 + V of position i at zero
@@ -106,16 +107,19 @@ template <int V>
 __device__ __forceinline__ Floats<V> masked(Floats<V> v, uint64_t seed, const Mask &m, int64_t i, int32_t j0)
 {
     const uint64_t first = seed + ((uint64_t)i * (uint64_t)m.words + (uint32_t)(j0 >> 2)) * kGolden;
-    const int shift = 16 * (j0 & 3);
     constexpr int kWords = (V + 3) / 4;
     uint64_t draws[kWords];
 #pragma unroll
     for (int w = 0; w < kWords; ++w) draws[w] = mix64(first + w * kGolden);
-    if (shift) {                                 // a piece that begins inside a word goes on in the next one
-        uint64_t next = 0;
-        if (shift + 16 * V > 64 * kWords) next = mix64(first + kWords * kGolden);
+    if (m.ragged) {
+        const int shift = 16 * (j0 & 3);
+        if (shift) {                             // the piece goes on in the next word
+            uint64_t next = 0;
+            if (shift + 16 * V > 64 * kWords) next = mix64(first + kWords * kGolden);
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) draws[w] = draws[w] >> shift | (w + 1 < kWords ? draws[w + 1 < kWords ? w + 1 : 0] : next) << (64 - shift);
+            for (int w = 0; w < kWords; ++w)
+                draws[w] = draws[w] >> shift | (w + 1 < kWords ? draws[w + 1 < kWords ? w + 1 : 0] : next) << (64 - shift);
+        }
     }
 #pragma unroll
     for (int e = 0; e < V; ++e)
