@@ -146,7 +146,8 @@ __device__ __forceinline__ uint32_t divided(const Div32 &by, uint32_t x, uint32_
 
 // One lane per piece of V elements; a workgroup takes kEmbedPieces * kBlock neighbouring pieces of the output in a turn.  Bound by
 // memory: slots, rows (random, each a few lines) and output.  2 M positions of 128 bf16 elements out of 25 M, 661 MB to move, by
-// pieces of a lane (2, 4, 8): 179 165 167 us; with 8, 32 and any number of workgroups for a compute unit 172 165 159.5 (4.1 TB/s).
+// pieces of a lane (2, 4, 8): 179 165 167 us; with 8, 32 and any number of workgroups for a compute unit 172 165 159.5;
+// with loads that no lane leaves out 157.5 (4.2 TB/s).
 constexpr int kEmbedPieces = 4;
 constexpr int64_t kEmbedBlocks = (int64_t)1 << 21;     // so that a turn's pieces fit 32 bits
 struct EmbedArgs {
@@ -182,7 +183,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a)
             uint32_t c;
             k[u] = k0 + divided(a.pieces, c0 + u * kBlock + threadIdx.x, &c);
             column[u] = (int32_t)c * V < a.dim - V ? (int32_t)c * V : a.dim - V;
-            slot[u] = i + u * kBlock < total ? a.slots[k[u]] : -1;
+            slot[u] = a.slots[k[u] < a.n ? k[u] : a.n - 1];      // (lanes behind the last piece store nothing)
         }
 #pragma unroll
         for (int u = 0; u < kEmbedPieces; ++u) {
