@@ -94,7 +94,8 @@ def tensor2d(rng, n, dim, dtype, layout="dense", scale=1.0):
 # ------------------------------------------------------------------------------------------------ lookup
 EMBED = [(1, 1, 1, F32, F32), (1, 7, 16, BF16, BF16), (2, 1, 3, F32, F16), (63, 10, 4, F16, F32), (64, 1000, 64, BF16, BF16),
          (257, 999, 50, F32, BF16), (1000, 50, 333, F16, F16), (333, 4099, 128, BF16, F32), (7, 100, 4096, BF16, BF16),
-         (5, 3, 5001, F32, F32), (20_011, 50_021, 48, F32, BF16), (100_003, 1000, 8, F16, BF16), (4097, 300, 1, BF16, F32)]
+         (5, 3, 5001, F32, F32), (20_011, 50_021, 48, F32, BF16), (100_003, 1000, 8, F16, BF16), (4097, 300, 1, BF16, F32),
+         (3, 2, 1 << 20, BF16, F32)]
 
 
 @pytest.mark.parametrize("n,num_rows,dim,table,out_type", EMBED)
@@ -201,7 +202,7 @@ GRAD = [(1, 1, 1, F32, F32), (1, 1000, 16, BF16, BF16), (2, 5, 3, F32, F32), (64
         (255, 255, 100, F32, BF16), (1024, 4096, 16, F32, F32), (2049, 65_535, 50, F16, F16), (4096, 256, 128, BF16, BF16),
         (4097, 255, 333, F32, F32), (1000, 77, 2048, BF16, F32), (300, 50, 4096, F32, F32), (129, 9, 5001, BF16, F32),
         (20_011, 50_021, 48, F32, F32), (65_537, 1_000_000, 64, BF16, F32), (140_001, 65_536, 4, F32, F32),
-        (300_007, 6_000_011, 8, BF16, BF16), (9000, (1 << 32) - 2, 32, F32, F32)]
+        (300_007, 6_000_011, 8, BF16, BF16), (9000, (1 << 32) - 2, 32, F32, F32), (3, 2, 1 << 20, BF16, F32)]
 
 
 @pytest.mark.parametrize("n,num_rows,dim,grad_type,out_type", GRAD)
@@ -328,6 +329,33 @@ def test_scratch_grows_and_keeps_what_it_had_room_for():
     rng = np.random.Generator(np.random.Philox(key=21))
     for n, dim in ((10, 4), (5000, 4), (100, 700), (70_000, 12), (3, 3000), (70_000, 16), (1, 1)):
         check_grad(h, draw_slots(rng, n, 50, "zipf"), tensor2d(rng, n, dim, F32), 50, F32, 1.0, 0.0, 0)
+    mp.mpzch_embed_destroy(h)
+
+
+def test_sums_of_gradients_and_tables_beyond_32_bits_of_bytes():
+    """Gradient rows and table rows behind the first 4 GiB; whole numbers, whose sums are exact."""
+    n, dim, num_rows = 8_700_001, 256, 1009
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    grad = torch.randint(-3, 4, (n, dim), generator=g, device="cuda", dtype=torch.int8).to(BF16)
+    slots = torch.randint(0, num_rows, (n,), generator=g, device="cuda")
+    want = torch.zeros(num_rows, dim, device="cuda")
+    for at in range(0, n, 1 << 20):
+        want.index_add_(0, slots[at:at + (1 << 20)], grad[at:at + (1 << 20)].float())
+    h = mp.mpzch_embed_create()
+    out_slots = torch.zeros(num_rows, dtype=torch.int64, device="cuda")
+    out_rows, count = torch.zeros(num_rows, dim, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    mp.mpzch_embed_grad(h, slots, grad, num_rows, out_slots, out_rows, count)
+    assert int(count.item()) == num_rows and torch.equal(out_slots, torch.arange(num_rows, device="cuda"))
+    assert torch.equal(out_rows, want)
+    del grad
+    many = 10_000_019
+    rows, far = torch.zeros(many, 128, device="cuda"), many - 1 - torch.arange(3000, device="cuda") * 3
+    slots, grad = far.repeat(4), torch.randint(-3, 4, (12_000, 128), generator=g, device="cuda").float()
+    mp.mpzch_embed_step(h, slots, grad, rows, None, torch.ones(1, device="cuda"))
+    assert torch.equal(rows[far], -grad.view(4, 3000, 128).sum(0))
+    rows[far] = 0
+    assert not rows.any()
     mp.mpzch_embed_destroy(h)
 
 
