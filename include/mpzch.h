@@ -478,7 +478,7 @@ mpzch_status_t mpzch_embed_reserve(mpzch_embed_t *h, int64_t max_n, int64_t max_
  * out_slots [dev] int64[out_cap], out_rows [dev] out_cap dense rows of dim elements of out_type (both may be NULL when
  *           out_cap == 0); entries from the count on are left as they were
  * out_count [dev] int64[1]: distinct rows; when it exceeds out_cap the lists hold the first out_cap
- * Errors: INVALID_ARG; UNSUPPORTED for num_rows > 2^32 - 2; ALLOC, HIP.
+ * Errors: INVALID_ARG; UNSUPPORTED for num_rows > 2^32 - 2 or a stride of 2^32 bytes or more; ALLOC, HIP.
  */
 mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t n, int64_t num_rows,
                                 const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,
@@ -489,7 +489,7 @@ mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t 
 /*
  * Optimizer step of the rows that the slots name, straight from the sums; other rows are not touched.
  * state [dev] float[num_rows] or NULL;  lr [dev] float[1], read on the device;  eps finite and > 0 where there is a state
- * Errors: INVALID_ARG; UNSUPPORTED for dim > MPZCH_MAX_STEP_DIM or num_rows > 2^32 - 2; ALLOC, HIP.
+ * Errors: INVALID_ARG; UNSUPPORTED for dim > MPZCH_MAX_STEP_DIM, num_rows > 2^32 - 2 or a stride of 2^32 bytes or more; ALLOC, HIP.
  */
 mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t n,
                                 const void *grad, int32_t grad_type, int64_t dim, int64_t grad_stride_bytes,

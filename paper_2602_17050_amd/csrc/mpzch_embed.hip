@@ -290,7 +290,7 @@ mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, i
     a.lanes = p.lanes;
     a.col_blocks = p.col_blocks;
     a.grad = (const char *)grad.at;
-    a.grad_stride = grad.stride;
+    a.grad_stride = (uint32_t)grad.stride;
     a.read_past_caches = n * grad.dim * element_bytes(grad.type) >= kReadPastCaches;
     a.tail_index = w.tail_index;
     a.arrived = w.arrived;
@@ -309,6 +309,7 @@ mpzch_status_t run_gradient(mpzch_embed_t *h, const int64_t *slots, int64_t n, i
 }
 
 constexpr int64_t kMaxGradRows = ((int64_t)1 << 32) - 2;     // rows and the padding behind them in 32 bits, one value to spare
+constexpr int64_t kMaxStride = ((int64_t)1 << 32) - 1;
 
 }  // namespace
 
@@ -378,7 +379,7 @@ mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t 
     if (!h || n < 0 || n > MPZCH_MAX_BATCH || num_rows < 1 || dim < 1 || dim > MPZCH_MAX_DIM || out_cap < 0 || !out_count)
         return MPZCH_ERR_INVALID_ARG;
     if (!type_ok(grad_type) || !type_ok(out_type)) return MPZCH_ERR_INVALID_ARG;
-    if (num_rows > kMaxGradRows) return MPZCH_ERR_UNSUPPORTED;
+    if (num_rows > kMaxGradRows || grad_stride_bytes > kMaxStride) return MPZCH_ERR_UNSUPPORTED;
     ReduceArgs a;
     std::memset(&a, 0, sizeof a);
     if (!make_mask(scale, drop_p, seed, dim, &a.factor, &a.mask)) return MPZCH_ERR_INVALID_ARG;
@@ -403,7 +404,8 @@ mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t 
 {
     if (!h || n < 0 || n > MPZCH_MAX_BATCH || num_rows < 1 || dim < 1 || !lr) return MPZCH_ERR_INVALID_ARG;
     if (!type_ok(grad_type) || !type_ok(rows_type)) return MPZCH_ERR_INVALID_ARG;
-    if (num_rows > kMaxGradRows || dim > MPZCH_MAX_STEP_DIM) return MPZCH_ERR_UNSUPPORTED;
+    if (num_rows > kMaxGradRows || dim > MPZCH_MAX_STEP_DIM || grad_stride_bytes > kMaxStride || row_stride_bytes > kMaxStride)
+        return MPZCH_ERR_UNSUPPORTED;
     if (state && !(std::isfinite(eps) && eps > 0.f)) return MPZCH_ERR_INVALID_ARG;
     ReduceArgs a;
     std::memset(&a, 0, sizeof a);
@@ -413,7 +415,8 @@ mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t 
     if (!w.ok()) return MPZCH_ERR_INVALID_ARG;
     if (n == 0) return MPZCH_OK;
     a.rows = (char *)rows;
-    a.row_stride = row_stride_bytes / element_bytes(rows_type);
+    a.row_stride = (uint32_t)row_stride_bytes;
+    a.per_element = 1.f / (float)dim;
     a.type = rows_type;
     a.state = state;
     a.lr = lr;

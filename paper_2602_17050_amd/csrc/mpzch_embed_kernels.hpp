@@ -106,7 +106,7 @@ struct Mask {
 template <int V>
 __device__ __forceinline__ Floats<V> masked(Floats<V> v, uint64_t seed, const Mask &m, int64_t i, int32_t j0)
 {
-    const uint64_t first = seed + ((uint64_t)i * (uint64_t)m.words + (uint32_t)(j0 >> 2)) * kGolden;
+    const uint64_t first = seed + ((uint64_t)(uint32_t)i * (uint32_t)m.words + (uint32_t)(j0 >> 2)) * kGolden;
     constexpr int kWords = (V + 3) / 4;
     uint64_t draws[kWords];
 #pragma unroll

@@ -106,7 +106,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
 #pragma unroll
             for (int p = 0; p < kColumns; ++p) {
                 const int32_t c = c0 + p * lanes + lane;
-                weight[p] = load_typed<1>(a.type, a.rows, (int64_t)row * a.row_stride + (c < col_end ? c : 0))[0];
+                weight[p] = load_typed<1>(a.type, a.rows + (uint64_t)row * a.row_stride, c < col_end ? c : 0)[0];
             }
         }
 #pragma unroll
@@ -157,7 +157,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
                 float all = 0.f;
 #pragma unroll
                 for (int w = 0; w < kReduceBlock / kWave; ++w) all += part[w];
-                state += all / (float)a.dim;
+                state += all * a.per_element;
                 if (threadIdx.x == 0) a.state[row] = state;
                 rate = lr / (sqrtf(state) + a.eps);
             }
@@ -165,8 +165,7 @@ __device__ __forceinline__ void join_run(const ReduceArgs &a, float *part, uint3
             for (int p = 0; p < kColumns; ++p) {
                 const int32_t c = c0 + p * lanes + lane;
                 if (c >= col_end || sharer != 0) continue;
-                const int64_t element = (int64_t)row * a.row_stride + c;
-                store_typed<1>(a.type, a.rows, element, Floats<1>(weight[p] - sum[p] * rate));
+                store_typed<1>(a.type, a.rows + (uint64_t)row * a.row_stride, c, Floats<1>(weight[p] - sum[p] * rate));
             }
         } else if (sharer == 0 && index < a.cap) {
             if (c0 == 0 && lane == 0) a.out_slots[index] = row;
@@ -277,7 +276,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     auto load_weights = [&](uint32_t row, Weights (&w)[NP], float &state) {
         state = a.state ? a.state[row] : 0.f;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) w[p].load(a.rows, (int64_t)row * a.row_stride + (column[p] < a.dim ? column[p] : 0));
+        for (int p = 0; p < NP; ++p) w[p].load(a.rows + (uint64_t)row * a.row_stride, column[p] < a.dim ? column[p] : 0);
     };
     // a finished sum
     auto emit_step = [&](uint32_t row, const Weights (&w)[NP], float state) {
@@ -302,21 +301,21 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
                     }
             }
             squares = group_sum(squares, a.lanes);
-            state += squares / (float)a.dim;
+            state += squares * a.per_element;
             if (lane == 0) a.state[row] = state;
             rate = lr / (sqrtf(state) + a.eps);
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p)
             if (column[p] < a.dim)
-                store_typed<V>(a.type, a.rows, (int64_t)row * a.row_stride + column[p], w[p].floats(a.type) - sum[p] * a.factor * rate);
+                store_typed<V>(a.type, a.rows + (uint64_t)row * a.row_stride, column[p], w[p].floats(a.type) - sum[p] * a.factor * rate);
     };
     auto emit_grad = [&](uint32_t row, uint32_t at) {
         if ((int64_t)at >= a.cap) return;
         if (block_col == 0 && lane == 0) a.out_slots[at] = row;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
-            if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)at * a.dim + column[p], sum[p] * a.factor, a.past_caches);
+            if (column[p] < a.dim) store_typed<V>(a.type, a.out_rows, (int64_t)((uint64_t)at * (uint32_t)a.dim) + column[p], sum[p] * a.factor, a.past_caches);
     };
     // (unconditional loads, so that all that are asked for are under way at a time: where nothing is wanted, of a row that is in the
     // caches anyway; a lane without columns has the first one)
@@ -324,7 +323,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     constexpr int kGradType = std::is_same_v<TG, float> ? kF32 : std::is_same_v<TG, __bf16> ? kBf16 : kF16;
     auto load_grad = [&](uint32_t at, Gradient (&g)[NP]) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) g[p].load(a.grad + (int64_t)at * a.grad_stride, column[p] < a.dim ? column[p] : 0);
+        for (int p = 0; p < NP; ++p) g[p].load(a.grad + (uint64_t)at * a.grad_stride, column[p] < a.dim ? column[p] : 0);
     };
     auto add = [&](const Gradient (&g)[NP], uint32_t at) {
 #pragma unroll
@@ -342,13 +341,14 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         Gradient g[kAhead][NP];
         Weights w[kAhead][NP];
         float state[kAhead];
-        uint32_t at[kAhead];
+        uint32_t at[kAhead], row[kAhead + 2];    // the entries' rows, and those before and behind them
+        bool counts[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead + 2; ++u) row[u] = row_of_entry[k0 + u];       // (behind the part: not looked at)
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int k = k0 + u < end ? k0 + u : end - 1;
-            const uint32_t row = row_of_entry[k + 1];
-            const bool wanted = row != a.num_rows && row != skipped;
-            at[u] = position[wanted ? k : 0];
+            counts[u] = k0 + u < end && row[u + 1] != a.num_rows && row[u + 1] != skipped;
+            at[u] = position[counts[u] ? k0 + u : 0];
         }
         if (a.read_past_caches) {
             asm volatile("" ::: "memory");       // (or the compiler makes plain loads of both)
@@ -356,32 +356,26 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             for (int u = 0; u < kAhead; ++u)
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
-                    g[u][p].load_past_caches(a.grad + (int64_t)at[u] * a.grad_stride, column[p] < a.dim ? column[p] : 0);
+                    g[u][p].load_past_caches(a.grad + (uint64_t)at[u] * a.grad_stride, column[p] < a.dim ? column[p] : 0);
             asm volatile("" ::: "memory");
         } else {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) load_grad(at[u], g[u]);
         }
+        if constexpr (STEP) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int k = k0 + u < end ? k0 + u : end - 1;
-            const uint32_t row = row_of_entry[k + 1];
-            const bool wanted = row != a.num_rows && row != skipped;
-            if constexpr (STEP) load_weights(wanted && row_of_entry[k + 2] != row ? row : 0, w[u], state[u]);
+            for (int u = 0; u < kAhead; ++u) load_weights(counts[u] && row[u + 2] != row[u + 1] ? row[u + 1] : 0, w[u], state[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int k = k0 + u;
-            if (k >= end) break;
-            const uint32_t row = row_of_entry[k + 1];
-            if (row == a.num_rows || row == skipped) {
+            if (!counts[u]) {
                 from_before = false;
                 continue;
             }
-            if (row_of_entry[k] != row) ++index;
+            if (row[u] != row[u + 1]) ++index;
             add(g[u], at[u]);
-            const bool goes_on = row_of_entry[k + 2] == row;
-            if (goes_on && k + 1 < end) continue;
+            const bool goes_on = row[u + 2] == row[u + 1];
+            if (goes_on && k0 + u + 1 < end) continue;
             if (from_before) {
                 flags |= kHeadShare | (goes_on ? kThrough : 0);
 #pragma unroll
@@ -389,9 +383,9 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
             } else if (goes_on) {
                 flags |= kTailShare;
             } else if constexpr (STEP) {
-                emit_step(row, w[u], state[u]);
+                emit_step(row[u + 1], w[u], state[u]);
             } else {
-                emit_grad(row, index - 1);
+                emit_grad(row[u + 1], index - 1);
             }
             from_before = false;
             if (!goes_on) {

@@ -15,7 +15,7 @@ struct ReduceArgs {
     int32_t lanes;               // of a group
     int32_t col_blocks;          // workgroups that share out the columns of a tile
     const char *grad;
-    int64_t grad_stride;
+    uint32_t grad_stride;        // bytes, as row_stride
     bool read_past_caches;       // grad is loaded non-temporally
     int32_t dim;
     float factor;
@@ -33,7 +33,8 @@ struct ReduceArgs {
     bool past_caches;            // out_rows are stored non-temporally
     // step
     char *rows;
-    int64_t row_stride;          // elements
+    uint32_t row_stride;
+    float per_element;           // 1 / dim
     float *state;
     const float *lr;
     float eps;

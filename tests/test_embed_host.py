@@ -79,6 +79,7 @@ def test_gradient_and_step_refuse_bad_arguments(binding):
                 dict(drop=0.1), dict(os_=None), dict(orr=None), dict(orr=odd), dict(g=odd), dict(ot=5), dict(cap=-1), dict(cnt=None)):
         assert grad(**bad) == INVALID, bad
     assert grad(nr=(1 << 32) - 1) == UNSUPPORTED
+    assert grad(gs=1 << 32) == UNSUPPORTED
 
     def step(h=h, slots=p, n=4, g=p, gt=F32, dim=16, gs=64, scale=1.0, drop=0.0, seed=None, rows=p, rt=F32, nr=10, rs=64, state=p,
              lr=p, eps=1e-6):
@@ -90,6 +91,7 @@ def test_gradient_and_step_refuse_bad_arguments(binding):
         assert step(**bad) == INVALID, bad
     assert step(dim=1025, gs=4100, rs=4100) == UNSUPPORTED
     assert step(nr=(1 << 32) - 1) == UNSUPPORTED
+    assert step(gs=1 << 32) == UNSUPPORTED and step(rs=1 << 32) == UNSUPPORTED
     assert step(n=0, slots=None, g=None) == 0
     assert lib.mpzch_embed_reserve(None, 1, 1) == INVALID
     for n, d in ((-1, 1), (1, -1), ((1 << 30) + 1, 1), (1, (1 << 20) + 1)):
