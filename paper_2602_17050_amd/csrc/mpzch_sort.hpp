@@ -235,11 +235,15 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const
     for (int u = 0; u < ITEMS; ++u) {
         const bool there = wave * (kWave * ITEMS) + u * kWave + lane < mine;
         const uint32_t digit = (uint32_t)(entry[u] >> s.shift) & (digits - 1);
-        uint64_t same = __ballot(there);
+        const uint64_t all_there = __ballot(there);
+        uint32_t low = (uint32_t)all_there, high = (uint32_t)(all_there >> 32);
         for (int b = 0; b < s.bits; ++b) {
-            const uint64_t set = __ballot(digit >> b & 1);
-            same &= digit >> b & 1 ? set : ~set;
+            const int32_t bit = (int32_t)(digit << (31 - b)) >> 31;        // all ones or zeros
+            const uint64_t set = __ballot(bit != 0);
+            low &= ~((uint32_t)set ^ (uint32_t)bit);
+            high &= ~((uint32_t)(set >> 32) ^ (uint32_t)bit);
         }
+        const uint64_t same = (uint64_t)high << 32 | low;
         const uint32_t at = (uint32_t)wave * digits + digit;
         const uint32_t so_far = count[at];
         place[u] = so_far + (uint32_t)__popcll(same & ((1ull << lane) - 1));
