@@ -98,15 +98,17 @@ constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
 struct Mask {
     const uint64_t *seed;
     uint32_t threshold;          // T; 0: no dropout
-    int32_t words;               // ceil(dim / 4)
+    uint64_t row_step;           // from one position's words to the next one's, in the generator: ceil(dim / 4) * kGolden
     int32_t ragged;              // whether pieces may begin inside a word: dim is no multiple of 4
 };
 
-// v with the dropped ones of the elements j0 .. j0 + V of position i at zero
+// the generator's state before the word of element j0 of position 0
+__device__ __forceinline__ uint64_t mask_column(uint64_t seed, int32_t j0) { return seed + (uint64_t)(uint32_t)(j0 >> 2) * kGolden; }
+// v with the dropped ones of the elements j0 .. j0 + V of position i at zero; at_column = mask_column(seed, j0)
 template <int V>
-__device__ __forceinline__ Floats<V> masked(Floats<V> v, uint64_t seed, const Mask &m, int64_t i, int32_t j0)
+__device__ __forceinline__ Floats<V> masked(Floats<V> v, uint64_t at_column, const Mask &m, uint32_t i, int32_t j0)
 {
-    const uint64_t first = seed + ((uint64_t)(uint32_t)i * (uint32_t)m.words + (uint32_t)(j0 >> 2)) * kGolden;
+    const uint64_t first = at_column + (uint64_t)i * m.row_step;
     constexpr int kWords = (V + 3) / 4;
     uint64_t draws[kWords];
 #pragma unroll
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a)
         for (int u = 0; u < kEmbedPieces; ++u) {
             if (i + u * kBlock >= total) continue;
             Floats<V> x = v[u].floats(std::is_same_v<TI, __bf16> ? kBf16 : kF16) * a.factor;
-            if constexpr (DROP) x = masked<V>(x, seed, a.mask, k[u], column[u]);
+            if constexpr (DROP) x = masked<V>(x, mask_column(seed, column[u]), a.mask, (uint32_t)k[u], column[u]);
             if (slot[u] < 0) x = Floats<V>(0.f);
             store_floats<TO, V>(a.out + k[u] * a.out_stride + (int64_t)column[u] * sizeof(TO), x, a.past_caches);
         }

@@ -267,6 +267,9 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
         column[p] = piece < a.dim ? (piece < a.dim - V ? piece : a.dim - V) : a.dim;
     }
     const uint64_t seed = a.mask.threshold ? *a.mask.seed : 0;
+    uint64_t mask_at[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) mask_at[p] = mask_column(seed, column[p]);
     const float lr = STEP ? *a.lr : 0.f;
     Floats<V> sum[NP];
 #pragma unroll
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const Floats<V> v = g[p].floats(kGradType);
-            sum[p] += a.mask.threshold ? masked<V>(v, seed, a.mask, at, column[p]) : v;
+            sum[p] += a.mask.threshold ? masked<V>(v, mask_at[p], a.mask, at, column[p]) : v;
         }
     };
 
