@@ -18,9 +18,9 @@ namespace {
 // the run's place alone determine: who is last does not change it.
 //
 // Bound by memory where batches are long: every gradient row is read once, 256 bytes and more at a random place.  2 M positions
-// of 128 bf16 elements (799 MB to move) take this kernel 214 us (3.7 TB/s; a copy 4.8), with distinct rows (1.55 GB) 381 (4.1), a
-// step of 1 M (394 MB) 118.  By round trips where they are short: entries, gradients and weights, shares.  65 536 positions with
-// a step (20 MB) 17 us, 1 024 7.
+// of 128 bf16 elements (799 MB to move) take this kernel 203 us (3.9 TB/s; a copy 4.8), a step of 1 M (394 MB) 108, and the vector
+// units are busy for nearly half of that.  By round trips where they are short: entries, gradients and weights, shares.  65 536
+// positions with a step (20 MB) 16 us, 1 024 7.
 constexpr int kBehind = 128;
 constexpr uint32_t kNoRow = ~0u;
 constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part

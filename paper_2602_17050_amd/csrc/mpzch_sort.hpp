@@ -27,8 +27,7 @@ __device__ __forceinline__ uint64_t sort_entry(const SortSource &s, int64_t i)
 
 // Short batches: an entry's place is the number of entries before it.  A workgroup counts for 16 entries, an entry in four lanes of each
 // of its 16 wavefronts, which have a 64th of the batch each.  n^2 comparisons, but one launch, and all compute units share them:
-// with the sums, gradients of 1 024 positions 11.6 us, 4 000 18, 8 000 28, where passes over digits take 29 (6 000 27 and 30); 10 000
-// 38 and 30.
+// with the sums, gradients of 1 024 positions 10.8 us, 4 000 18, 8 000 28, where passes over digits take 29; 10 000 38 and 30.
 constexpr int kRankMax = 8192;
 constexpr int kRanked = 16, kRankParts = kSortBlock / kRanked;
 __global__ __launch_bounds__(kSortBlock) void k_sort_rank(const int64_t *slots, RowMod mod, int32_t n, uint64_t *out)
