@@ -527,7 +527,9 @@ __global__ __launch_bounds__(kReduceBlock) void k_reduce(ReduceArgs a)
     };
     if (unfinished) {
         keep(part, sum);
-        if (lane == 0 && block_col == 0) store_shared(a.tail_index + tile_index, index - 1);
+        // by the workgroup of every block of columns, the same value: arrivals are counted for each block by itself, so the last one
+        // of a block sees what its own owner stored before it arrived, and nothing of another block's
+        if (lane == 0) store_shared(a.tail_index + tile_index, index - 1);
     }
     if (has_head) keep(part + NP * V * a.lanes, chain);
     __syncthreads();

@@ -23,7 +23,7 @@ struct ReduceArgs {
     // shares of the tiles, tiles x dim each: of a run that began before, and of one that begins in the tile
     float *head, *tail;
     uint32_t *tail_index;        // of the run that begins in the tile, among all
-    uint32_t *arrived;           // shares of the run that begins in the tile; zero between the calls
+    uint32_t *arrived;           // shares of the run that begins in the tile, for each block of columns; zero between the calls
     const uint32_t *heads;       // runs that begin in a tile, or (heads_are == kBeforeTile) in all tiles before
     int32_t heads_are;
     // gradient

@@ -586,3 +586,26 @@ def test_binding_refuses_tensors_that_do_not_fit(handle):
             mp.mpzch_embed(slots, rows, out, scale=scale, drop_p=p)
         assert e.value.status == 1
     assert not out.any() and not rows.any()
+
+
+# ------------------------------------------------------------------------------------------------ what went wrong before
+@pytest.mark.parametrize("dim,dtype", [(1025, BF16), (2048, BF16), (4100, F32), (16_384, BF16)])
+def test_long_runs_of_rows_of_many_column_blocks_go_to_their_own_place(dim, dtype):
+    """Rows of more than 1 024 elements are shared out over workgroups by columns, and each of them joins its columns of a long run by
+    itself.  Where the run is in the list changes from call to call on one handle, from a scratch that nothing has used on: every
+    block of columns has to take this call's place.  Sums of small whole numbers are exact."""
+    rng = np.random.Generator(np.random.Philox(key=dim))
+    n, num_rows = 4500, 9000
+    h = mp.mpzch_embed_create()
+    for k, single in enumerate((0, 700, 3, 250, 1500, 0)):      # rows of one position in front of the long runs
+        long_rows = 2000 + 7 * np.arange(3) + k
+        lengths = np.array([1100, 900, n - single - 2000])
+        slots_np = np.concatenate([np.arange(single), np.repeat(long_rows, lengths)]).astype(np.int64)
+        slots_np = slots_np[rng.permutation(n)]
+        grad_np = rng.integers(-4, 5, size=(n, dim)).astype(np.float32)
+        say("long runs", dim, dtype, k, single)
+        got_slots, got_rows, count = run_grad(h, slots_np, torch.from_numpy(grad_np).cuda().to(dtype), num_rows, F32, 1.0, 0.0, 0, cap=2000)
+        named, total, _, _ = ref.sums(slots_np, grad_np, num_rows, 1.0, 0.0, 0)
+        assert count == len(named) == single + 3 and np.array_equal(got_slots[:count], named)
+        assert np.array_equal(f64(got_rows)[:count], total) and (f64(got_rows)[count:] == -77).all()
+    mp.mpzch_embed_destroy(h)
