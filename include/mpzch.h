@@ -442,7 +442,7 @@ mpzch_status_t mpzch_lookup_jagged(mpzch_group_t *g, const int64_t *const *ident
  * grad, out  [dev] n rows of dim elements of grad_type / out_type, grad_stride_bytes / out_stride_bytes apart: the
  *            block of one table in a wider activation will do.  Element alignment is enough everywhere; dim a multiple of
  *            8 (4 with 32-bit elements) on 16-byte boundaries is the fastest.
- * scale      finite;  drop_p in [0, 1];  seed [dev] uint64[1], may be NULL where T is 0
+ * scale      finite, and f too in 32 bits;  drop_p in [0, 1];  seed [dev] uint64[1], may be NULL where T is 0
  * Products and sums are formed in 32-bit floats and rounded once, to nearest, to the type of the result; the order of a
  * sum is determined by n, dim, the types, the tensors' alignment and the slots: the same call gives the same bits.
  * No output may overlap an input (of a step: rows and state are updated in place).

@@ -69,7 +69,7 @@ bool make_mask(float scale, double drop_p, const int64_t *seed, int64_t dim, flo
     mask->row_step = (uint64_t)((dim + 3) / 4) * kGolden;
     mask->ragged = dim % 4 != 0;
     *factor = t == 65536 ? 0.f : (float)((double)scale * 65536.0 / (65536.0 - t));
-    return true;
+    return std::isfinite(*factor);               // (0 * infinity: NaN where kept terms sum to zero)
 }
 
 // ---- lookup ---------------------------------------------------------------------------------

@@ -118,3 +118,21 @@ def test_reference_step_by_hand():
 def test_entry_points_are_public(name):
     import paper_2602_17050_amd as pkg
     assert callable(getattr(pkg, name))
+
+
+def test_a_factor_beyond_32_bit_floats_is_refused(binding):
+    """scale * 65536 / (65536 - T) is held in 32 bits: an infinite one would make NaN of elements that are zero."""
+    lib = binding.load_library()
+    p = ctypes.c_void_p(0x10000)                              # never dereferenced: every call below fails first
+    h = binding.mpzch_embed_create()
+    top = float(np.finfo(np.float32).max)
+    for scale, drop in ((3e38, 0.5), (-3e38, 0.5), (2e38, 1 / 3 + 0.1), (1e34, 65535 / 65536), (top, 1 / 65536)):
+        assert abs(ref.factor(scale, drop)) > top and abs(scale) <= top
+        assert lib.mpzch_embed(p, 4, p, F32, 10, 16, 64, scale, drop, p, p, F32, 64, None) == INVALID, (scale, drop)
+        assert lib.mpzch_embed(None, 0, None, F32, 10, 16, 64, scale, drop, p, None, F32, 64, None) == INVALID, (scale, drop)
+        assert lib.mpzch_embed_grad(h, p, 4, 10, p, F32, 16, 64, scale, drop, p, p, p, F32, 4, p, None) == INVALID, (scale, drop)
+        assert lib.mpzch_embed_step(h, p, 4, p, F32, 16, 64, scale, drop, p, p, F32, 10, 64, p, p, 1e-6, None) == INVALID, (scale, drop)
+    # the largest scale alone, and one that the growth leaves finite; everything dropped has no growth
+    for scale, drop in ((top, 0.0), (1.5e38, 0.5), (top, 1.0)):
+        assert lib.mpzch_embed(None, 0, None, F32, 10, 16, 64, scale, drop, p, None, F32, 64, None) == 0, (scale, drop)
+    binding.mpzch_embed_destroy(h)
