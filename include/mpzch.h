@@ -489,6 +489,7 @@ mpzch_status_t mpzch_embed_grad(mpzch_embed_t *h, const int64_t *slots, int64_t 
 /*
  * Optimizer step of the rows that the slots name, straight from the sums; other rows are not touched.
  * state [dev] float[num_rows] or NULL;  lr [dev] float[1], read on the device;  eps finite and > 0 where there is a state
+ * (subnormal too: lr / (sqrt(state) + eps) need not fit 32 bits, and sums of zero change nothing, for any |lr| below 2^78)
  * Errors: INVALID_ARG; UNSUPPORTED for dim > MPZCH_MAX_STEP_DIM, num_rows > 2^32 - 2 or a stride of 2^32 bytes or more; ALLOC, HIP.
  */
 mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t n,

@@ -609,3 +609,45 @@ def test_long_runs_of_rows_of_many_column_blocks_go_to_their_own_place(dim, dtyp
         assert count == len(named) == single + 3 and np.array_equal(got_slots[:count], named)
         assert np.array_equal(f64(got_rows)[:count], total) and (f64(got_rows)[count:] == -77).all()
     mp.mpzch_embed_destroy(h)
+
+
+@pytest.mark.parametrize("dim", [1, 16, 50, 600])
+@pytest.mark.parametrize("lr,eps,state_exp,grad_exp", [
+    (1.0, 2.0 ** -149, None, None), (0.5, 1e-44, None, None), (1e30, 1e-10, None, None), (0.0, 2.0 ** -149, None, None),
+    (1e30, 1e-12, -60, -40), (2.0 ** 127, 2.0 ** -126, -60, -60), (1e-30, 1e-6, 60, 40), (-1e30, 1e-12, -60, -40)])
+def test_rates_beyond_32_bit_floats(handle, dim, lr, eps, state_exp, grad_exp):
+    """lr / (sqrt(state) + eps) need not fit 32 bits where lr G / (sqrt(state) + eps) does.  Sums of zero (terms of zero, terms that
+    cancel, everything dropped) change nothing, whatever lr and eps; others change the rows by what the formula says.  Rows of one
+    position, of a few, and of thousands, which a whole workgroup adds up.
+
+    With a sum G of terms of absolute sum S: tolerances of the step above, from weights of zero; the change stays above 2^-126."""
+    rng = np.random.Generator(np.random.Philox(key=dim))
+    lr, eps = float(np.float32(lr)), float(np.float32(eps))
+    slots_np = np.concatenate([np.arange(40), np.repeat([50, 51], 30), np.repeat([60, 61], 2600)]).astype(np.int64)
+    n, num_rows = len(slots_np), 64
+    zero = state_exp is None
+    grad_np = rng.integers(1, 5, size=(n, dim)).astype(np.float64) * 2.0 ** (0 if zero else grad_exp)
+    if zero:
+        grad_np[:40] = 0
+        grad_np[1::2] = -grad_np[::2]                            # (pairs of neighbours, which are of one row)
+    order = rng.permutation(n)
+    slots_np, grad_np = slots_np[order], grad_np[order]
+    grad = torch.from_numpy(grad_np).cuda().float()
+    rows = torch.from_numpy(rng.standard_normal((num_rows, dim)) if zero else np.zeros((num_rows, dim))).cuda().float()
+    state = torch.full((num_rows,), 0.0 if zero else 2.0 ** state_exp, device="cuda")
+    before, state_before = rows.clone(), state.clone()
+    say("rates", dim, lr, eps, state_exp)
+    mp.mpzch_embed_step(handle, torch.from_numpy(slots_np).cuda(), grad, rows, state, torch.full((1,), lr, device="cuda"), eps)
+    if zero:
+        assert torch.equal(rows, before) and torch.equal(state, state_before)
+        mp.mpzch_embed_step(handle, torch.from_numpy(slots_np).cuda(), torch.full_like(grad, 3.0), rows, state,
+                            torch.full((1,), lr, device="cuda"), eps, drop_p=1.0, seed=seed_tensor(5))
+        assert torch.equal(rows, before) and torch.equal(state, state_before)
+        return
+    named, total, size, terms = ref.sums(slots_np, f64(grad), num_rows, 1.0, 0.0, 0)
+    want, want_state = ref.step(f64(before), f64(state_before), named, total, lr, eps)
+    e_g = (terms[:, None] + 2) * U * size
+    e_state, e_change = adagrad_errors(total, e_g, f64(state_before)[named], want_state[named], abs(lr), eps)
+    assert (np.abs(want[named]) > 2.0 ** -126).all() and (np.abs(want[named]) < 2.0 ** 127).all()
+    close(f64(state)[named], want_state[named], 1.01 * e_state, "state")
+    close(f64(rows)[named], want[named], 1.01 * (e_change + 5 * U * np.abs(want[named])), "rows")
