@@ -264,7 +264,8 @@ def mpzch_apply_delta(identities, slots, ids, count_dev, rows=None, delta_rows=N
 
 def mpzch_embed(slots, rows, out, scale: float = 1.0, drop_p: float = 0.0, seed=None):
     """out[i] = rows[slots[i] mod len(rows)], scaled, dropped with probability drop_p and converted; zeros for a negative slot.
-    rows, out: 2-D device tensors with dense rows (float32, bfloat16 or float16 each); seed: int64[1] on the device."""
+    rows, out: 2-D device tensors with dense rows (float32, bfloat16 or float16 each); seed: int64[1] on the device.
+    Not an autograd function (mpzch_embed_grad is its gradient): where gradients are enabled, rows that require one are refused."""
     status = (_native or _load_native()).embed(slots, rows, out, scale, drop_p, seed)
     if status:
         raise MpzchError(status, "mpzch_embed")
@@ -288,7 +289,8 @@ def mpzch_embed_reserve(handle, max_n: int, max_dim: int):
 def mpzch_embed_grad(handle, slots, grad, num_rows: int, out_slots, out_rows, out_count, scale: float = 1.0,
                      drop_p: float = 0.0, seed=None):
     """The gradient of mpzch_embed for its output's gradient: out_slots[:k] the distinct rows that slots name, ascending,
-    out_rows[:k] their sums, out_count[0] = k."""
+    out_rows[:k] their sums, out_count[0] = k.  Not an autograd function: where gradients are enabled, a grad that requires one is
+    refused."""
     status = (_native or _load_native()).embed_grad(handle, slots, grad, num_rows, out_slots, out_rows, out_count, scale, drop_p, seed)
     if status:
         raise MpzchError(status, "mpzch_embed_grad")

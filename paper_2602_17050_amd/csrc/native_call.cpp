@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/Tensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -326,6 +327,12 @@ void here(const at::Tensor &t)
 {
     if (!t.is_cuda() || t.device().index() != c10::hip::current_device()) fail(PyExc_AssertionError, "tensors on the current device only");
 }
+// The calls are no autograd functions: a gradient that would be lost in silence is an error.
+void no_gradient(PyObject *o)
+{
+    if (c10::GradMode::is_enabled() && tensor(o).requires_grad())
+        fail(PyExc_AssertionError, "this call has no gradient of its own: detach() the tensor, or call under torch.no_grad() or inside an autograd function");
+}
 template <typename T>
 T *dense(PyObject *o, at::ScalarType type, int64_t numel, const char *text)
 {
@@ -384,6 +391,7 @@ PyObject *embed(PyObject *const *a)
     int64_t n;
     const int64_t *slots = slots_of(a[0], &n);
     const Typed rows(a[1]), out(a[2]);
+    no_gradient(a[1]);
     if (out.n != n || out.dim != rows.dim) fail(PyExc_AssertionError, "out: one row per slot, as long as the table's");
     return call(g_call.mpzch_embed, slots, n, (const void *)rows.at, rows.type, rows.n, rows.dim, rows.stride, (float)real(a[3]),
                 real(a[4]), seed_of(a[5]), out.at, out.type, out.stride, stream());
@@ -394,6 +402,7 @@ PyObject *embed_grad(PyObject *const *a)
     int64_t n;
     const int64_t *slots = slots_of(a[1], &n);
     const Typed grad(a[2]), rows(a[5]);
+    no_gradient(a[2]);
     if (grad.n != n) fail(PyExc_AssertionError, "grad: one row per slot");
     if (rows.dim != grad.dim || rows.stride != rows.dim * (rows.type == MPZCH_F32 ? 4 : 2)) fail(PyExc_AssertionError, "out_rows: dense rows as long as the gradient's");
     int64_t *out_slots = dense<int64_t>(a[4], at::kLong, rows.n, "out_slots: one dense int64 per row of out_rows");

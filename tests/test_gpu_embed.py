@@ -651,3 +651,52 @@ def test_rates_beyond_32_bit_floats(handle, dim, lr, eps, state_exp, grad_exp):
     assert (np.abs(want[named]) > 2.0 ** -126).all() and (np.abs(want[named]) < 2.0 ** 127).all()
     close(f64(state)[named], want_state[named], 1.01 * e_state, "state")
     close(f64(rows)[named], want[named], 1.01 * (e_change + 5 * U * np.abs(want[named])), "rows")
+
+
+def test_lookup_and_gradient_refuse_to_lose_a_gradient(handle):
+    """Neither is differentiable by itself: with gradients enabled, rows or gradients that require one are refused, not detached
+    in silence.  Without (torch.no_grad(), detach(), the inside of an autograd function) the same tensors do."""
+    slots = torch.tensor([1, 0, 1], device="cuda")
+    weight = torch.nn.Parameter(torch.randn(4, 8, device="cuda"))
+    out, count = torch.zeros(3, 8, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    with pytest.raises(AssertionError, match="gradient"):
+        mp.mpzch_embed(slots, weight, out)
+    with pytest.raises(AssertionError, match="gradient"):
+        mp.mpzch_embed(slots, weight * 2, out)
+    out_slots, out_rows = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, 8, device="cuda")
+    needs = torch.ones(3, 8, device="cuda", requires_grad=True)
+    with pytest.raises(AssertionError, match="gradient"):
+        mp.mpzch_embed_grad(handle, slots, needs, 4, out_slots, out_rows, count)
+    assert not out.any() and not count.any()
+    mp.mpzch_embed(slots, weight.detach(), out)
+    assert torch.equal(out, weight[slots])
+    out.zero_()
+    with torch.no_grad():
+        mp.mpzch_embed(slots, weight, out)
+        mp.mpzch_embed_grad(handle, slots, needs, 4, out_slots, out_rows, count)
+    assert torch.equal(out, weight[slots]) and int(count.item()) == 2
+
+    class Lookup(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, rows, at):
+            ctx.save_for_backward(at)
+            ctx.shape = rows.shape
+            result = torch.empty(at.numel(), rows.shape[1], device="cuda")
+            mp.mpzch_embed(at, rows, result, scale=2.0)
+            return result
+
+        @staticmethod
+        def backward(ctx, g):
+            (at,) = ctx.saved_tensors
+            named = torch.zeros(at.numel(), dtype=torch.int64, device="cuda")
+            sums, k = torch.zeros(at.numel(), ctx.shape[1], device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+            mp.mpzch_embed_grad(handle, at, g.contiguous(), ctx.shape[0], named, sums, k, scale=2.0)
+            whole = torch.zeros(ctx.shape, device="cuda")
+            m = int(k.item())
+            whole[named[:m]] = sums[:m]
+            return whole, None
+
+    c = torch.randint(-3, 4, (3, 8), device="cuda").float()
+    (Lookup.apply(weight, slots) * c).sum().backward()
+    want = torch.zeros(4, 8, device="cuda").index_add_(0, slots, 2 * c)
+    assert torch.equal(weight.grad, want)
