@@ -333,6 +333,17 @@ void no_gradient(PyObject *o)
     if (c10::GradMode::is_enabled() && tensor(o).requires_grad())
         fail(PyExc_AssertionError, "this call has no gradient of its own: detach() the tensor, or call under torch.no_grad() or inside an autograd function");
 }
+// ... and what they write is a new version of the tensor, which autograd notices if it kept the old one (tensors of inference mode
+// have none)
+template <typename... O>
+PyObject *wrote(PyObject *status, O... tensors)
+{
+    auto written = [](PyObject *o) {
+        if (o != Py_None && !tensor(o).is_inference()) tensor(o).unsafeGetTensorImpl()->bump_version();
+    };
+    if (status && PyLong_AsLong(status) == MPZCH_OK) (written(tensors), ...);
+    return status;
+}
 template <typename T>
 T *dense(PyObject *o, at::ScalarType type, int64_t numel, const char *text)
 {
@@ -393,8 +404,8 @@ PyObject *embed(PyObject *const *a)
     const Typed rows(a[1]), out(a[2]);
     no_gradient(a[1]);
     if (out.n != n || out.dim != rows.dim) fail(PyExc_AssertionError, "out: one row per slot, as long as the table's");
-    return call(g_call.mpzch_embed, slots, n, (const void *)rows.at, rows.type, rows.n, rows.dim, rows.stride, (float)real(a[3]),
-                real(a[4]), seed_of(a[5]), out.at, out.type, out.stride, stream());
+    return wrote(call(g_call.mpzch_embed, slots, n, (const void *)rows.at, rows.type, rows.n, rows.dim, rows.stride, (float)real(a[3]),
+                real(a[4]), seed_of(a[5]), out.at, out.type, out.stride, stream()), a[2]);
 }
 // handle, slots, grad, num_rows, out_slots, out_rows, out_count, scale, drop_p, seed
 PyObject *embed_grad(PyObject *const *a)
@@ -408,8 +419,8 @@ PyObject *embed_grad(PyObject *const *a)
     int64_t *out_slots = dense<int64_t>(a[4], at::kLong, rows.n, "out_slots: one dense int64 per row of out_rows");
     if (a[6] == Py_None) fail(PyExc_AssertionError, "out_count: one int64 on the device");
     int64_t *out_count = dense<int64_t>(a[6], at::kLong, 1, "out_count: one int64 on the device");
-    return call(g_call.mpzch_embed_grad, handle<mpzch_embed_t>(a[0]), slots, n, number(a[3]), (const void *)grad.at, grad.type, grad.dim,
-                grad.stride, (float)real(a[7]), real(a[8]), seed_of(a[9]), out_slots, rows.at, rows.type, rows.n, out_count, stream());
+    return wrote(call(g_call.mpzch_embed_grad, handle<mpzch_embed_t>(a[0]), slots, n, number(a[3]), (const void *)grad.at, grad.type, grad.dim,
+                grad.stride, (float)real(a[7]), real(a[8]), seed_of(a[9]), out_slots, rows.at, rows.type, rows.n, out_count, stream()), a[4], a[5], a[6]);
 }
 // handle, slots, grad, rows, state, lr, eps, scale, drop_p, seed
 PyObject *embed_step(PyObject *const *a)
@@ -420,9 +431,9 @@ PyObject *embed_step(PyObject *const *a)
     if (grad.n != n || grad.dim != rows.dim) fail(PyExc_AssertionError, "grad: one row per slot, as long as the table's");
     float *state = dense<float>(a[4], at::kFloat, rows.n, "state: one dense float32 per row");
     const float *lr = dense<const float>(a[5], at::kFloat, 1, "lr: one float32 on the device");
-    return call(g_call.mpzch_embed_step, handle<mpzch_embed_t>(a[0]), slots, n, (const void *)grad.at, grad.type, grad.dim, grad.stride,
+    return wrote(call(g_call.mpzch_embed_step, handle<mpzch_embed_t>(a[0]), slots, n, (const void *)grad.at, grad.type, grad.dim, grad.stride,
                 (float)real(a[7]), real(a[8]), seed_of(a[9]), rows.at, rows.type, rows.n, rows.stride, state, lr, (float)real(a[6]),
-                stream());
+                stream()), a[3], a[4]);
 }
 
 template <PyObject *(*FN)(PyObject *const *), int N>

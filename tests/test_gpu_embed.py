@@ -700,3 +700,30 @@ def test_lookup_and_gradient_refuse_to_lose_a_gradient(handle):
     (Lookup.apply(weight, slots) * c).sum().backward()
     want = torch.zeros(4, 8, device="cuda").index_add_(0, slots, 2 * c)
     assert torch.equal(weight.grad, want)
+
+
+def test_what_is_written_gets_a_new_version(handle):
+    """Autograd notices that a tensor which it keeps for a backward pass was written over."""
+    slots = torch.tensor([1, 0, 1], device="cuda")
+    rows, state, lr = torch.randn(4, 8, device="cuda"), torch.zeros(4, device="cuda"), torch.ones(1, device="cuda")
+    out, count = torch.zeros(3, 8, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    out_slots, out_rows = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, 8, device="cuda")
+    read = (slots, lr)
+    read_before = [t._version for t in read]
+    for call, written in ((lambda: mp.mpzch_embed(slots, rows, out), (out,)),
+                          (lambda: mp.mpzch_embed_grad(handle, slots, out, 4, out_slots, out_rows, count), (out_slots, out_rows, count)),
+                          (lambda: mp.mpzch_embed_step(handle, slots, out, rows, state, lr), (rows, state)),
+                          (lambda: mp.mpzch_embed_step(handle, slots, out, rows, None, lr), (rows,))):
+        before = [t._version for t in written]
+        call()
+        assert all(t._version > b for t, b in zip(written, before))
+    assert [t._version for t in read] == read_before
+    weight = torch.randn(4, 8, device="cuda", requires_grad=True)
+    loss = (weight * weight).sum()                               # (keeps the weight)
+    mp.mpzch_embed_step(handle, slots, out, weight, None, lr)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        kept = torch.zeros(3, 8, device="cuda")
+    mp.mpzch_embed(slots, rows, kept)                            # (tensors of inference mode have no version)
+    assert torch.equal(kept, rows[slots])
