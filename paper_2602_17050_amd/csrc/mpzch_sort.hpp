@@ -246,9 +246,10 @@ __global__ __launch_bounds__(kSortBlock) void k_sort_scatter(SortSource s, const
         const uint32_t at = (uint32_t)wave * digits + digit;
         const uint32_t so_far = count[at];
         place[u] = so_far + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        __builtin_amdgcn_wave_barrier();
+        // (no instruction: the hardware does a wavefront's accesses in order, the compiler is kept from moving any across)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (there && (same >> lane) == 1) count[at] = (uint16_t)(place[u] + 1);       // the last of them
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
     {
