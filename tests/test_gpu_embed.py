@@ -727,3 +727,61 @@ def test_what_is_written_gets_a_new_version(handle):
         kept = torch.zeros(3, 8, device="cuda")
     mp.mpzch_embed(slots, rows, kept)                            # (tensors of inference mode have no version)
     assert torch.equal(kept, rows[slots])
+
+
+def fenced(n, dim, dtype, values=None):
+    """(the whole tensor, n x dim of it): rows that begin at the fourth element of wider ones, with a sentinel in front of, between and
+    behind them that none of the operators writes"""
+    whole = torch.full((n + 2, dim + 7), 1536.0, dtype=dtype, device="cuda")
+    view = whole[1:-1, 3:3 + dim]
+    if values is not None:
+        view.copy_(values)
+    return whole, view
+
+
+def assert_fence_stands(whole, dim):
+    inside = torch.zeros_like(whole, dtype=torch.bool)
+    inside[1:-1, 3:3 + dim] = True
+    assert bool((whole.float()[~inside] == 1536.0).all())
+
+
+@pytest.mark.parametrize("dim", [1, 2, 3, 5, 7, 8, 9, 15, 50, 129, 511, 1001, 1024, 1025, 2051])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_nothing_in_front_of_or_behind_the_rows_is_touched(handle, dim, dtype):
+    """The last piece of a row whose length is no multiple of a piece is moved back towards the row's begin; padding and dropped elements
+    write zeros.  Neither reaches beyond the row, and single rows, of some positions and of thousands, are where they should be."""
+    rng = np.random.Generator(np.random.Philox(key=dim))
+    n, num_rows = 3000, 300
+    slots_np = draw_slots(rng, n, num_rows, "zipf")
+    slots_np[:1200] = 7
+    slots_np[5] = -1
+    slots_np = slots_np[rng.permutation(n)]
+    slots = torch.from_numpy(slots_np).cuda()
+    table = rng.integers(-8, 9, size=(num_rows, dim)).astype(np.float32)
+    whole_rows, rows = fenced(num_rows, dim, dtype, torch.from_numpy(table))
+    whole_out, out = fenced(n, dim, dtype)
+    say("fence", dim, dtype)
+    mp.mpzch_embed(slots, rows, out, scale=2.0, drop_p=0.5, seed=seed_tensor(6))
+    assert np.array_equal(f64(out), ref.embed(slots_np, table.astype(np.float64), 2.0, 0.5, 6))
+    assert_fence_stands(whole_out, dim)
+    assert_fence_stands(whole_rows, dim)
+    grad_np = rng.integers(-1, 2, size=(n, dim)).astype(np.float32)
+    whole_grad, grad = fenced(n, dim, dtype, torch.from_numpy(grad_np))
+    sums = torch.full((num_rows + 2, dim), 1536.0, device="cuda")
+    named, total, _, _ = ref.sums(slots_np, grad_np, num_rows, 1.0, 0.5, 6)
+    out_slots, count = torch.zeros(num_rows, dtype=torch.int64, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    mp.mpzch_embed_grad(handle, slots, grad, num_rows, out_slots, sums[1:-1], count, drop_p=0.5, seed=seed_tensor(6))
+    k = int(count.item())
+    assert k == len(named) and np.array_equal(out_slots[:k].cpu().numpy(), named) and np.array_equal(f64(sums)[1:1 + k], total)
+    assert bool((sums[0] == 1536.0).all()) and bool((sums[1 + k:] == 1536.0).all())
+    assert_fence_stands(whole_grad, dim)
+    if dim > 1024:
+        return
+    state = torch.full((num_rows + 2,), 1536.0, device="cuda")
+    state[1:-1] = 0
+    for s in (None, state[1:-1]):
+        mp.mpzch_embed_step(handle, slots, grad, rows, s, torch.full((1,), 0.5, device="cuda"), 1e-6, drop_p=0.5, seed=seed_tensor(6))
+        assert_fence_stands(whole_rows, dim)
+    assert float(state[0]) == 1536.0 and float(state[-1]) == 1536.0
+    untouched = np.setdiff1d(np.arange(num_rows), named)
+    assert np.array_equal(f64(rows)[untouched], table[untouched]) and not f64(state)[1:-1][untouched].any()
