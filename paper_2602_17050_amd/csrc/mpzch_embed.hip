@@ -82,7 +82,9 @@ template <typename TI, typename TO>
 mpzch_status_t launch_embed(const EmbedArgs &a, int width, int grid, hipStream_t s)
 {
     switch (width) {
-    case 8: return launch_embed<TI, TO, 8>(a, grid, s);
+    case 8:
+        if constexpr (sizeof(TI) == 2 && sizeof(TO) == 2) return launch_embed<TI, TO, 8>(a, grid, s);
+        return MPZCH_ERR_UNSUPPORTED;
     case 4: return launch_embed<TI, TO, 4>(a, grid, s);
     case 2: return launch_embed<TI, TO, 2>(a, grid, s);
     default: return launch_embed<TI, TO, 1>(a, grid, s);

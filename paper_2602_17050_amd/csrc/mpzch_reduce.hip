@@ -611,7 +611,10 @@ mpzch_status_t launch_reduce(const ReduceArgs &a, int width, int pieces, int gri
         if constexpr (sizeof(TG) == 2)
             return pieces == 1 ? launch(k_reduce<TG, 8, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 8, 2, WB>, grid, kReduceBlock, s, a);
         return MPZCH_ERR_UNSUPPORTED;
-    case 4: return pieces == 1 ? launch(k_reduce<TG, 4, 1, WB>, grid, kReduceBlock, s, a) : launch(k_reduce<TG, 4, 4, WB>, grid, kReduceBlock, s, a);
+    case 4:
+        if constexpr (sizeof(TG) == 4)           // (16 bits: rows of four to seven elements)
+            if (pieces != 1) return launch(k_reduce<TG, 4, 4, WB>, grid, kReduceBlock, s, a);
+        return launch(k_reduce<TG, 4, 1, WB>, grid, kReduceBlock, s, a);
     case 2: return launch(k_reduce<TG, 2, 1, WB>, grid, kReduceBlock, s, a);       // (rows of three elements, or two)
     default: return launch(k_reduce<TG, 1, 1, WB>, grid, kReduceBlock, s, a);
     }
