@@ -50,12 +50,13 @@ int piece_width(int64_t dim, int32_t type, int32_t other)
     return width;
 }
 
-// Results of this many bytes are stored past the caches.  With a kernel behind that reads them, us, through / past: lookups of 8 MB
-// 11.9 / 12.0, 33 MB 23.7 / 23.1, 77 MB 45.0 / 44.4, 180 MB 119.8 / 119.7.
+// Results of this many bytes are stored past the caches.  Together with a kernel behind that reads them and writes as much, us, through /
+// past: lookups of 33 MB 23.7 / 23.2, 77 MB 44.2 / 43.8, 179 MB 110 / 118 (the memory-side cache would have held them for the
+// reader), 512 MB 336 / 327; of 8 MB, through the caches, 12.0.
 constexpr int64_t kPastCaches = (int64_t)1 << 24;
 // Gradients of this many bytes are read past the caches, of which the rest of the program keeps more that way: half of the memory-side
-// one, since what a backward pass has just written may still be there.  Sums of 512 MB 298 / 289 us, a step from 256 MB 175 / 168;
-// of 38 MB, which the cache did hold, 62 / 65.
+// one, since what a backward pass has just written may still be there.  us, through / past: sums of 512 MB 290.5 / 280, a step from
+// 256 MB 171.7 / 164.5; of 33 and 38 MB, which the cache did hold, 37.2 / 38.5 and 59.2 / 62.3.
 constexpr int64_t kReadPastCaches = (int64_t)1 << 27;
 
 // scale and dropout of a call
@@ -418,6 +419,7 @@ mpzch_status_t mpzch_embed_step(mpzch_embed_t *h, const int64_t *slots, int64_t 
     if (n == 0) return MPZCH_OK;
     a.rows = (char *)rows;
     a.row_stride = (uint32_t)row_stride_bytes;
+    // (one more rounding of the mean than a division by dim, half a step, where dim is no power of two: the sum has dim of them)
     a.per_element = 1.f / (float)dim;
     a.type = rows_type;
     a.state = state;

@@ -33,8 +33,8 @@ __device__ __forceinline__ Floats<V> load_floats(const char *at)
     return __builtin_convertvector(*reinterpret_cast<const Pack<E, V> *>(at), Floats<V>);
 }
 // Rounded once, to nearest, ties to even.  past_caches: non-temporally, so that large results do not drive out of the caches what
-// is read again.  Lookup of 2 M rows of 256 bytes 172 -> 125 us, gradient of as many (271 MB of sums) 302 -> 297; non-temporal
-// loads of rows: 219.
+// is read again.  Of three tables in turn, us, through / past: lookup of 2 M rows of 256 bytes 164 / 157.4 (and with non-temporal loads
+// of the table's rows 179), of 33 MB 10.6 / 9.8, gradient of 2 M rows (271 MB of sums) 288.5 / 280.
 template <typename E, int V>
 __device__ __forceinline__ void store_floats(char *at, Floats<V> v, bool past_caches = false)
 {

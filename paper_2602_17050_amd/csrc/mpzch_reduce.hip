@@ -15,12 +15,13 @@ namespace {
 // A run that goes on behind the tile for kBehind entries at most is finished there, by all groups of the workgroup in which it
 // is, and the following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to
 // write one is found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and
-// the run's place alone determine: who is last does not change it.
+// the run's place alone determine: who is last does not change it.  (Against 64 bits they are off by 4e-8 to 5e-8 of the gradient's
+// size; sums in 64 bits, rounded to 32 at the end, by 2e-8 to 3e-8: twice the registers for less than a bit.)
 //
 // Bound by memory where batches are long: every gradient row is read once, 256 bytes and more at a random place.  2 M positions
-// of 128 bf16 elements (799 MB to move) take this kernel 203 us (3.9 TB/s; a copy 4.8), a step of 1 M (394 MB) 108, and the vector
+// of 128 bf16 elements (799 MB to move) take this kernel 202 us (4.0 TB/s; a copy 4.8), a step of 1 M (394 MB) 109, and the vector
 // units are busy for nearly half of that.  By round trips where they are short: entries, gradients and weights, shares.  65 536
-// positions with a step (20 MB) 16 us, 1 024 7.
+// positions with a step (20 MB) 16 us, 1 024 7 to 8.
 constexpr int kBehind = 128;
 constexpr uint32_t kNoRow = ~0u;
 constexpr uint32_t kHeadShare = 1, kThrough = 2, kTailShare = 4;      // flags of a part
