@@ -16,7 +16,7 @@ namespace {
 // is, and the following tiles leave it out.  A longer one has a share in memory for every tile; which workgroup is the last to
 // write one is found with a counter, and that one adds them up.  All sums are in 32 bits, in an order that n, dim, the types and
 // the run's place alone determine: who is last does not change it.  (Against 64 bits they are off by 4e-8 to 5e-8 of the gradient's
-// size; sums in 64 bits, rounded to 32 at the end, by 2e-8 to 3e-8: twice the registers for less than a bit.)
+// size; sums in 64 bits, rounded to 32 at the end, by 2e-8 to 3e-8: twice the registers for about one bit.)
 //
 // Bound by memory where batches are long: every gradient row is read once, 256 bytes and more at a random place.  2 M positions
 // of 128 bf16 elements (799 MB to move) take this kernel 202 us (4.0 TB/s; a copy 4.8), a step of 1 M (394 MB) 109, and the vector
